@@ -76,9 +76,10 @@ enum {
     MDRAFT_DT_SOFTPLUS = 1u,  /* Delta = softplus(dt + dt_bias); otherwise Delta = dt + dt_bias as given        */
     MDRAFT_PRECONV     = 2u,  /* x already is u = SiLU(conv(x)): skip the conv, leave conv windows untouched    */
     MDRAFT_CONV_ONLY   = 4u,  /* write u to `out`, advance the conv window, do not run the recurrence           */
-    MDRAFT_A_POWERS    = 8u   /* caller asserts A[d][n] == (n+1)*A[d][0] exactly in fp32 (e.g. the S4D-real
+    MDRAFT_A_POWERS    = 8u,  /* caller asserts A[d][n] == (n+1)*A[d][0] exactly in fp32 (e.g. the S4D-real
                                  initialisation -(1..N)): decays are then formed from ONE exponential per
                                  token and channel by repeated multiplication.  mdraft_classify_A checks it. */
+    MDRAFT_BETA_SIGMOID = 16u /* delta layers: beta = sigmoid of what is passed; otherwise beta as given */
 };
 
 /* bits ORed into *dev_status by kernels */
@@ -425,6 +426,110 @@ int mdraft_ssd_tree_step(const mdraft_ssd_layer *layer, const mdraft_cache *cach
                          int32_t *dev_status, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------------------
+ * Gated delta rule drafter layer.  Like Mamba-2 a recurrent layer with one decay per head and a state of constant size, so it
+ * drafts the way the paper's drafter does (Section 3.1 encode, Section 4.1 tree); what a token writes is the difference between
+ * its value and what the state already holds for its key.  Per value head j (key head j / (n_v_heads / n_k_heads)), with the
+ * state S a d_v x d_k matrix:
+ *
+ *     alpha_t = exp( softplus(dt[t][j] + dt_bias[j]) * A[j] )                 (MDRAFT_DT_SOFTPLUS; else exp((dt + dt_bias) A))
+ *     beta_t  = sigmoid( beta[t][j] )                                         (MDRAFT_BETA_SIGMOID; else as given)
+ *     r       = beta_t * ( v_t - alpha_t * S_{t-1} k_t )
+ *     S_t     = alpha_t * S_{t-1} + r k_t^T
+ *     o_t     = scale * S_t q_t
+ *     out_t   = [ o_t / sqrt(mean(o_t^2) + eps) * norm_w ]  [ * SiLU(z_t) ]      (rounded to the activation type)
+ *
+ * The bracketed parts are left out where norm_w / z is NULL.  q, k and v are taken as given: a block convolves its q | k | v
+ * channels with a MDRAFT_CONV_ONLY call over a layer of that many channels (the same state pool holds the windows) and brings
+ * the query and key heads to unit length with mdraft_qk_norm.  Keys have to keep beta * |k|^2 at 2 or less, as unit keys do: with larger ones the
+ * recurrence itself grows without bound.
+ *
+ * Supported: d_k and d_v 64 or 128, n_v_heads a multiple of n_k_heads, fp32 or bf16 activations; anything else is
+ * MDRAFT_ERR_UNSUPPORTED.  State slots: (n_v_heads * d_v, d_k) fp32 in an mdraft_cache, whose windows these calls do not touch (cache->conv may
+ * be NULL).  flags: MDRAFT_DT_SOFTPLUS, MDRAFT_BETA_SIGMOID.
+ */
+typedef struct {
+    int32_t n_k_heads, n_v_heads, d_k, d_v;
+    int32_t act;            /* mdraft_dtype of q, k, v, z, dt, beta, out */
+    uint32_t flags;
+    float scale;            /* of the outputs, d_k^-1/2 as a rule */
+    float eps;              /* of the output norm */
+    const float *A;         /* (n_v_heads), <= 0 */
+    const float *dt_bias;   /* (n_v_heads) or NULL for 0 */
+    const float *norm_w;    /* (d_v) or NULL: no output norm */
+} mdraft_gdr_layer;
+
+/*
+ * Context encode of a delta layer over packed sequences.
+ *   q, k      : (T, n_k_heads * d_k), strides ldq, ldk          v, z, out : (T, n_v_heads * d_v), strides ldv, ldz, ldo; z may be NULL
+ *   dt, beta  : (T, n_v_heads), strides lddt, ldbeta (elements; any value >= n_v_heads)
+ *   cu_seqlens, init_slot, final_slot, dev_status, stream: as in mdraft_conv_scan_prefill (cu_seqlens may be NULL for one sequence), but
+ *   no sequence may start from another's final_slot, however long it is.  init_slot[s] == final_slot[s] is allowed.  Rows that belong to no sequence
+ *   are neither read into a result nor written
+ *   max_seqlen: an upper bound on the longest sequence (HOST value): with its help the call chooses how it works; the results do not
+ *               depend on it beyond rounding
+ *   workspace : device scratch of at least mdraft_gdr_prefill_workspace_bytes(...) bytes, 256-byte aligned; NULL where that is 0.  `out` must not
+ *               overlap an input
+ */
+size_t mdraft_gdr_prefill_workspace_bytes(const mdraft_gdr_layer *layer, int32_t total_tokens, int32_t n_seq, int32_t max_seqlen);
+
+int mdraft_gdr_prefill(const mdraft_gdr_layer *layer, const mdraft_cache *cache, int32_t layer_index,
+                       const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *z, int64_t ldz,
+                       const void *dt, int64_t lddt, const void *beta, int64_t ldbeta, void *out, int64_t ldo,
+                       int32_t total_tokens, int32_t n_seq, int32_t max_seqlen,
+                       const int32_t *cu_seqlens, const int32_t *init_slot, const int32_t *final_slot,
+                       void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * Draft-tree step of a delta layer: one token for each node of a level, node i from slot parent_slot[i] (-1: the zero state) into slot
+ * node_slot[i] (paper Section 4.1, as mdraft_tree_step).  q, k: (M, n_k_heads * d_k); v, z, out: (M, n_v_heads * d_v); dt, beta:
+ * (M, n_v_heads).  Levels, hazards (early input rows included) and device-side faults as in mdraft_tree_step.  All arithmetic is fp32.
+ */
+int mdraft_gdr_tree_step(const mdraft_gdr_layer *layer, const mdraft_cache *cache, int32_t layer_index,
+                         const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v, int64_t ldv, const void *z, int64_t ldz,
+                         const void *dt, int64_t lddt, const void *beta, int64_t ldbeta, void *out, int64_t ldo,
+                         int32_t n_nodes, const int32_t *parent_slot, const int32_t *node_slot,
+                         int32_t n_levels, const int32_t *level_offsets, int32_t *dev_status, void *stream);
+
+/*
+ * Norm of every query and key head, with the position rotation in the same pass.  Per row and head of d_head values
+ *
+ *     y = x / sqrt(mean(x^2) + eps) * w      (MDRAFT_NORM_RMS)
+ *     y = x / sqrt(sum(x^2) + eps) * w       (MDRAFT_NORM_L2)
+ *     y = x                                  (MDRAFT_NORM_NONE)
+ *
+ * with w = q_w or k_w (NULL: 1), then for i < rot_dim / 2 the pair (a, b) = (y[i], y[i + rot_dim/2]) (MDRAFT_ROT_HALF) or
+ * (y[2i], y[2i+1]) (MDRAFT_ROT_PAIRS) becomes
+ *
+ *     (a cos t - b sin t, b cos t + a sin t) * rot_scale,      t = positions[row] * freqs[i]
+ *
+ * and the values from rot_dim on stay as the norm left them.  Arithmetic is fp32, rounded once at the end; t is formed and
+ * reduced in 64 bits, so far positions lose nothing.  Contexts stretched by other frequencies come with their own `freqs` (and rot_scale).  A
+ * tree node's position is its sequence's length plus its depth.
+ *   q, q_out : (rows, n_q_heads * d_head), strides ldq, ldqo      k, k_out : (rows, n_k_heads * d_head), strides ldk, ldko
+ *              q_out may be q with the same stride, k_out likewise (in place); no other overlap.  One of the head counts may be 0
+ *   positions: (rows) int32, may be NULL when rot_dim is 0
+ * Supported: d_head a multiple of 8 up to 256; rot_dim even and at most d_head, a multiple of 16 for MDRAFT_ROT_HALF; fp32 or bf16
+ * activations; anything else is MDRAFT_ERR_UNSUPPORTED.  No counterpart in the paper, which does not look inside a layer.
+ */
+enum { MDRAFT_NORM_NONE = 0, MDRAFT_NORM_L2 = 1, MDRAFT_NORM_RMS = 2 };
+enum { MDRAFT_ROT_HALF = 0, MDRAFT_ROT_PAIRS = 1 };
+
+typedef struct {
+    int32_t d_head, n_q_heads, n_k_heads;
+    int32_t act;            /* mdraft_dtype of q, k and the results */
+    int32_t norm;           /* MDRAFT_NORM_* */
+    int32_t rot_dim;        /* rotated values of a head, 0 = none */
+    int32_t rot_layout;     /* MDRAFT_ROT_* */
+    float eps, rot_scale;
+    const float *q_w, *k_w; /* (d_head) or NULL */
+    const float *freqs;     /* (rot_dim / 2) radians per position */
+} mdraft_qk_norm_spec;
+
+int mdraft_qk_norm(const mdraft_qk_norm_spec *spec, const void *q, int64_t ldq, const void *k, int64_t ldk,
+                   void *q_out, int64_t ldqo, void *k_out, int64_t ldko, const int32_t *positions, int32_t n_rows, void *stream);
+
+/*
  * Accepted-path commit: for j in [0, n_commit) and every layer of the cache,
  * slot dst_slot[j] <- slot src_slot[j] (SSM state and conv window), bit for
  * bit.  After verification the drafter continues from the state of the last
@@ -436,6 +541,13 @@ int mdraft_ssd_tree_step(const mdraft_ssd_layer *layer, const mdraft_cache *cach
 int mdraft_state_commit(const mdraft_cache *cache, int32_t d_inner, int32_t d_state, int32_t d_conv, int32_t act,
                         int32_t n_commit, const int32_t *src_slot, const int32_t *dst_slot,
                         int32_t *dev_status, void *stream);
+
+/*
+ * The same for slots whose state and window differ in width, as a delta layer's do: the state is (d_inner, d_state) fp32 with d_state 64
+ * or 128, the window (d_conv - 1, conv_channels) activations.  conv_channels 0: the pool has no windows (cache->conv may be NULL).
+ */
+int mdraft_gdr_state_commit(const mdraft_cache *cache, int32_t d_inner, int32_t d_state, int32_t conv_channels, int32_t d_conv, int32_t act,
+                            int32_t n_commit, const int32_t *src_slot, const int32_t *dst_slot, int32_t *dev_status, void *stream);
 
 /*
  * Checks on the device whether A (D x N, fp32) satisfies A[d][n] == (n+1)*A[d][0]

@@ -12,6 +12,8 @@ from .binding import (  # noqa: F401
     mdraft_classify_A, mdraft_conv_scan_prefill, mdraft_conv_scan_prefill_noalloc, mdraft_prefill_workspace_bytes,
     NOALLOC_SCRATCH_BYTES, mdraft_conv_scan_prefill_stack, mdraft_prefill_stack_launches, mdraft_prefill_stack_workspace_bytes,
     mdraft_tree_step_stack, mdraft_block_generation,
+    MDRAFT_BETA_SIGMOID, MDRAFT_NORM_NONE, MDRAFT_NORM_L2, MDRAFT_NORM_RMS, MDRAFT_ROT_HALF, MDRAFT_ROT_PAIRS,
+    GdrLayer, mdraft_gdr_prefill, mdraft_gdr_prefill_workspace_bytes, mdraft_gdr_tree_step, mdraft_gdr_state_commit, QkNorm, mdraft_qk_norm,
     SsdLayer, mdraft_ssd_prefill, mdraft_ssd_prefill_workspace_bytes, mdraft_ssd_tree_step,
     mdraft_state_commit, mdraft_tree_step, mdraft_tree_step_proj, mdraft_version, status_string,
 )

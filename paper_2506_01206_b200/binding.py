@@ -22,7 +22,10 @@ LIB_PATH = os.path.join(_HERE, "libmdraft.so")
 MDRAFT_F32, MDRAFT_BF16 = 0, 1
 MDRAFT_ERR_WORKSPACE = -4
 MDRAFT_DT_SOFTPLUS, MDRAFT_PRECONV, MDRAFT_CONV_ONLY, MDRAFT_A_POWERS = 1, 2, 4, 8
+MDRAFT_BETA_SIGMOID = 16
 MDRAFT_DEV_BAD_SLOT, MDRAFT_DEV_BAD_SEQLENS, MDRAFT_DEV_WAIT_EXPIRED = 1, 2, 4
+MDRAFT_NORM_NONE, MDRAFT_NORM_L2, MDRAFT_NORM_RMS = 0, 1, 2
+MDRAFT_ROT_HALF, MDRAFT_ROT_PAIRS = 0, 1
 
 EXPORTS = (
     "mdraft_prefill_workspace_bytes", "mdraft_conv_scan_prefill", "mdraft_conv_scan_prefill_noalloc", "mdraft_tree_step",
@@ -31,6 +34,7 @@ EXPORTS = (
     "mdraft_ssd_prefill_workspace_bytes", "mdraft_ssd_prefill", "mdraft_ssd_tree_step",
     "mdraft_prefill_stack_workspace_bytes", "mdraft_prefill_stack_launches", "mdraft_conv_scan_prefill_stack", "mdraft_tree_step_stack",
     "mdraft_block_generation",
+    "mdraft_gdr_prefill_workspace_bytes", "mdraft_gdr_prefill", "mdraft_gdr_tree_step", "mdraft_gdr_state_commit", "mdraft_qk_norm",
 )
 
 
@@ -68,6 +72,17 @@ class _SsdLayer(C.Structure):
                 ("A", C.c_void_p), ("D", C.c_void_p), ("conv_w", C.c_void_p), ("conv_b", C.c_void_p), ("dt_bias", C.c_void_p)]
 
 
+class _GdrLayer(C.Structure):
+    _fields_ = [("n_k_heads", C.c_int32), ("n_v_heads", C.c_int32), ("d_k", C.c_int32), ("d_v", C.c_int32), ("act", C.c_int32),
+                ("flags", C.c_uint32), ("scale", C.c_float), ("eps", C.c_float), ("A", C.c_void_p), ("dt_bias", C.c_void_p), ("norm_w", C.c_void_p)]
+
+
+class _QkNormSpec(C.Structure):
+    _fields_ = [("d_head", C.c_int32), ("n_q_heads", C.c_int32), ("n_k_heads", C.c_int32), ("act", C.c_int32), ("norm", C.c_int32),
+                ("rot_dim", C.c_int32), ("rot_layout", C.c_int32), ("eps", C.c_float), ("rot_scale", C.c_float),
+                ("q_w", C.c_void_p), ("k_w", C.c_void_p), ("freqs", C.c_void_p)]
+
+
 class _Ucb(C.Structure):
     _fields_ = [("n_arms", C.c_int32), ("reserved", C.c_int32), ("round", C.c_int64), ("lambda_ucb", C.c_double),
                 ("lambda_gamma", C.c_double), ("reward_sum", C.POINTER(C.c_double)), ("count", C.POINTER(C.c_int64))]
@@ -98,7 +113,8 @@ except ImportError:   # the package has to be importable for its own build
 # entry points whose arguments csrc/host.cpp marshals, in the order of its table
 _HOST_CALLS = ("mdraft_conv_scan_prefill", "mdraft_conv_scan_prefill_noalloc", "mdraft_tree_step", "mdraft_tree_step_proj",
                "mdraft_state_commit", "mdraft_ssd_prefill", "mdraft_ssd_tree_step", "mdraft_conv_scan_prefill_stack",
-               "mdraft_tree_step_stack", "mdraft_block_generation")
+               "mdraft_tree_step_stack", "mdraft_block_generation", "mdraft_gdr_prefill", "mdraft_gdr_tree_step", "mdraft_gdr_state_commit",
+               "mdraft_qk_norm")
 
 
 def load_library(path: Optional[str] = None):
@@ -157,6 +173,18 @@ def load_library(path: Optional[str] = None):
     lib.mdraft_ssd_tree_step.argtypes = [C.POINTER(_SsdLayer), C.POINTER(_Cache), i32,
                                          vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
                                          i32, vp, vp, i32, C.POINTER(i32), vp, vp]
+    lib.mdraft_gdr_prefill_workspace_bytes.restype = C.c_size_t
+    lib.mdraft_gdr_prefill_workspace_bytes.argtypes = [C.POINTER(_GdrLayer), i32, i32, i32]
+    lib.mdraft_gdr_prefill.restype = C.c_int
+    lib.mdraft_gdr_prefill.argtypes = [C.POINTER(_GdrLayer), C.POINTER(_Cache), i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                       i32, i32, i32, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    lib.mdraft_gdr_tree_step.restype = C.c_int
+    lib.mdraft_gdr_tree_step.argtypes = [C.POINTER(_GdrLayer), C.POINTER(_Cache), i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                         i32, vp, vp, i32, C.POINTER(i32), vp, vp]
+    lib.mdraft_gdr_state_commit.restype = C.c_int
+    lib.mdraft_gdr_state_commit.argtypes = [C.POINTER(_Cache), i32, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.mdraft_qk_norm.restype = C.c_int
+    lib.mdraft_qk_norm.argtypes = [C.POINTER(_QkNormSpec), vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp]
     # The calls that are issued once per layer go through the extension, which is given the addresses of this library.
     if isinstance(_host, _NotBuilt):
         _host = _load_host()
@@ -231,13 +259,15 @@ class Layer:
 
 
 class StateCache:
-    """Slot pool: ssm (n_layers, n_slots, D, N) fp32 and conv (n_layers, n_slots, W-1, D) activations."""
+    """Slot pool: ssm (n_layers, n_slots, D, N) fp32 and conv (n_layers, n_slots, W-1, D) activations.  `conv_channels`: channels of
+    the windows where they are not D (a delta layer convolves its q | k | v channels)."""
 
     def __init__(self, n_layers: int, n_slots: int, d_inner: int, d_state: int = 16, d_conv: int = 4,
-                 act: torch.dtype = torch.bfloat16, device="cuda", zero: bool = True):
+                 act: torch.dtype = torch.bfloat16, device="cuda", zero: bool = True, conv_channels: Optional[int] = None):
         alloc = torch.zeros if zero else torch.empty
+        self.conv_channels = d_inner if conv_channels is None else int(conv_channels)
         self.ssm = alloc((n_layers, n_slots, d_inner, d_state), dtype=torch.float32, device=device)
-        self.conv = alloc((n_layers, n_slots, d_conv - 1, d_inner), dtype=act, device=device)
+        self.conv = alloc((n_layers, n_slots, d_conv - 1, self.conv_channels), dtype=act, device=device)
         self.n_layers, self.n_slots, self.d_inner, self.d_state, self.d_conv, self.act = n_layers, n_slots, d_inner, d_state, d_conv, act
 
     def c(self) -> _Cache:
@@ -371,6 +401,9 @@ def mdraft_tree_step_proj(layer: Layer, cache: StateCache, layer_index: int, W_x
 
 def mdraft_state_commit(cache: StateCache, src_slot: torch.Tensor, dst_slot: torch.Tensor,
                         dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    if cache is not None and (cache.conv_channels != cache.d_inner or cache.d_state == 64):   # slots of a delta layer
+        mdraft_gdr_state_commit(cache, src_slot, dst_slot, dev_status, stream)
+        return
     rc = _host.commit(_entry(), cache, src_slot, dst_slot, dev_status, stream)
     if rc != 0:
         raise MdraftError(rc, "mdraft_state_commit")
@@ -477,3 +510,89 @@ def mdraft_ssd_tree_step(layer: SsdLayer, cache: StateCache, layer_index: int, x
                              stream, flags)
     if rc != 0:
         raise MdraftError(rc, "mdraft_ssd_tree_step")
+
+
+# ---------------------------------------------------------------- gated delta rule layer
+@dataclass
+class GdrLayer:
+    """Constants of a delta layer on the device (fp32): A (Hv,), dt_bias (Hv,) or None, norm_w (d_v,) or None for no output norm."""
+    A: torch.Tensor
+    dt_bias: Optional[torch.Tensor]
+    norm_w: Optional[torch.Tensor]
+    n_k_heads: int
+    d_k: int = 128
+    d_v: int = 128
+    act: torch.dtype = torch.bfloat16
+    flags: int = MDRAFT_DT_SOFTPLUS | MDRAFT_BETA_SIGMOID
+    scale: Optional[float] = None
+    eps: float = 1e-5
+
+    def __post_init__(self):
+        H = int(self.A.numel())
+        _f32(self.A, H, "A"); _f32(self.dt_bias, H, "dt_bias"); _f32(self.norm_w, self.d_v, "norm_w")
+        if self.scale is None:
+            self.scale = self.d_k ** -0.5
+        self.n_v_heads, self.d_inner, self.d_state = H, H * self.d_v, self.d_k
+
+    def c(self, flags: Optional[int] = None) -> _GdrLayer:
+        return _GdrLayer(self.n_k_heads, self.n_v_heads, self.d_k, self.d_v, _act_of(self.act), self.flags if flags is None else int(flags),
+                         self.scale, self.eps, self.A.data_ptr(), 0 if self.dt_bias is None else self.dt_bias.data_ptr(),
+                         0 if self.norm_w is None else self.norm_w.data_ptr())
+
+
+def mdraft_gdr_prefill_workspace_bytes(layer: GdrLayer, total_tokens: int, n_seq: int, max_seqlen: int) -> int:
+    cl = layer.c()
+    return int(load_library().mdraft_gdr_prefill_workspace_bytes(C.byref(cl), int(total_tokens), int(n_seq), int(max_seqlen)))
+
+
+def mdraft_gdr_prefill(layer: GdrLayer, cache: Optional[StateCache], layer_index: int, q, k, v, z, dt, beta, out,
+                       cu_seqlens: Optional[torch.Tensor], max_seqlen: int, init_slot: Optional[torch.Tensor] = None,
+                       final_slot: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                       dev_status: Optional[torch.Tensor] = None, stream=None, flags: Optional[int] = None) -> None:
+    rc = _host.gdr_prefill(_entry(), layer, cache, layer_index, q, k, v, z, dt, beta, out, cu_seqlens, max_seqlen, init_slot, final_slot, workspace,
+                           dev_status, stream, flags)
+    if rc != 0:
+        raise MdraftError(rc, "mdraft_gdr_prefill")
+
+
+def mdraft_gdr_tree_step(layer: GdrLayer, cache: StateCache, layer_index: int, q, k, v, z, dt, beta, out,
+                         parent_slot: torch.Tensor, node_slot: torch.Tensor, level_offsets: Optional[Sequence[int]] = None,
+                         dev_status: Optional[torch.Tensor] = None, stream=None, flags: Optional[int] = None) -> None:
+    rc = _host.gdr_tree_step(_entry(), layer, cache, layer_index, q, k, v, z, dt, beta, out, parent_slot, node_slot, level_offsets, dev_status,
+                             stream, flags)
+    if rc != 0:
+        raise MdraftError(rc, "mdraft_gdr_tree_step")
+
+
+def mdraft_gdr_state_commit(cache: StateCache, src_slot: torch.Tensor, dst_slot: torch.Tensor,
+                            dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """What mdraft_state_commit calls for a pool whose windows are as wide as `cache.conv_channels`."""
+    rc = _host.gdr_commit(_entry(), cache, src_slot, dst_slot, dev_status, stream)
+    if rc != 0:
+        raise MdraftError(rc, "mdraft_gdr_state_commit")
+
+
+@dataclass
+class QkNorm:
+    """What mdraft_qk_norm does to a row's heads.  Weights (d_head,) and frequencies (rot_dim / 2,) are fp32 on the device."""
+    d_head: int
+    n_q_heads: int
+    n_k_heads: int
+    act: torch.dtype = torch.bfloat16
+    norm: int = MDRAFT_NORM_L2
+    q_w: Optional[torch.Tensor] = None
+    k_w: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+    rot_dim: int = 0
+    rot_layout: int = MDRAFT_ROT_HALF
+    freqs: Optional[torch.Tensor] = None
+    rot_scale: float = 1.0
+
+    def __post_init__(self):
+        _f32(self.q_w, self.d_head, "q_w"); _f32(self.k_w, self.d_head, "k_w"); _f32(self.freqs, self.rot_dim // 2, "freqs")
+
+
+def mdraft_qk_norm(spec: QkNorm, q, k, q_out, k_out, positions: Optional[torch.Tensor] = None, stream=None) -> None:
+    rc = _host.qk_norm(_entry(), spec, q, k, q_out, k_out, positions, stream)
+    if rc != 0:
+        raise MdraftError(rc, "mdraft_qk_norm")

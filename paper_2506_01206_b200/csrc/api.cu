@@ -10,8 +10,10 @@
 #include "block.cuh"
 #include "commit.cuh"
 #include "common.cuh"
+#include "gdr.cuh"
 #include "prefill.cuh"
 #include "prefill_cluster.cuh"
+#include "qk_norm.cuh"
 #include "ssd.cuh"
 #include "tree_proj.cuh"
 #include "tree_step.cuh"
@@ -982,6 +984,176 @@ int mdraft_ssd_tree_step(const mdraft_ssd_layer* layer, const mdraft_cache* cach
         ++a.level_in_call;
     }
     return MDRAFT_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------------- delta layer
+namespace {
+
+int check_gdr_layer(const mdraft_gdr_layer* L) {
+    if (!L || !L->A || L->n_k_heads <= 0 || L->n_v_heads <= 0) return MDRAFT_ERR_INVALID_ARG;
+    if ((L->d_k != 64 && L->d_k != 128) || (L->d_v != 64 && L->d_v != 128) || L->n_v_heads % L->n_k_heads != 0 || L->n_v_heads > 4096 ||
+        (L->act != MDRAFT_F32 && L->act != MDRAFT_BF16))
+        return MDRAFT_ERR_UNSUPPORTED;
+    if (L->flags & ~(uint32_t)(MDRAFT_DT_SOFTPLUS | MDRAFT_BETA_SIGMOID)) return MDRAFT_ERR_INVALID_ARG;
+    return MDRAFT_OK;
+}
+
+// A pool whose windows are of no interest to the call.
+int check_states(const mdraft_cache* c, int64_t elems, int layer_index) {
+    if (!c || !c->ssm) return MDRAFT_ERR_INVALID_ARG;
+    if (c->n_layers <= 0 || c->n_slots <= 0 || layer_index < 0 || layer_index >= c->n_layers) return MDRAFT_ERR_INVALID_ARG;
+    if (c->ssm_slot_stride < elems || (c->n_layers > 1 && c->ssm_layer_stride < 0)) return MDRAFT_ERR_INVALID_ARG;
+    if (!aligned16(c->ssm) || (c->ssm_slot_stride * 4) % 16 || (c->ssm_layer_stride * 4) % 16) return MDRAFT_ERR_MISALIGNED;
+    return MDRAFT_OK;
+}
+
+int check_gdr_io(const mdraft_gdr_layer* L, const GdrIo& io, bool have_rows) {
+    const int dk = L->n_k_heads * L->d_k, dv = L->n_v_heads * L->d_v;
+    int rc;
+    if ((rc = check_matrix(io.q, io.ldq, dk, L->act, have_rows))) return rc;
+    if ((rc = check_matrix(io.k, io.ldk, dk, L->act, have_rows))) return rc;
+    if ((rc = check_matrix(io.v, io.ldv, dv, L->act, have_rows))) return rc;
+    if ((rc = check_matrix(io.z, io.ldz, dv, L->act, false))) return rc;
+    if ((rc = check_matrix(io.out, io.ldo, dv, L->act, have_rows))) return rc;
+    if (have_rows && (!io.dt || io.lddt < L->n_v_heads || !io.beta || io.ldb < L->n_v_heads)) return MDRAFT_ERR_INVALID_ARG;
+    return MDRAFT_OK;
+}
+
+GdrLayerDev gdr_layer_dev(const mdraft_gdr_layer* L) {
+    GdrLayerDev d;
+    d.A = L->A; d.dt_bias = L->dt_bias; d.norm_w = L->norm_w;
+    d.n_k_heads = L->n_k_heads; d.n_v_heads = L->n_v_heads; d.flags = L->flags; d.scale = L->scale; d.eps = L->eps;
+    return d;
+}
+
+PoolDev states_dev(const mdraft_cache* c, int layer_index) {
+    PoolDev p = {};
+    if (!c) return p;
+    p.ssm = c->ssm + (int64_t)layer_index * c->ssm_layer_stride;
+    p.ssm_slot_stride = c->ssm_slot_stride;
+    p.n_slots = c->n_slots;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mdraft_gdr_prefill_workspace_bytes(const mdraft_gdr_layer* layer, int32_t total_tokens, int32_t n_seq, int32_t max_seqlen) {
+    return 0;
+}
+
+int mdraft_gdr_prefill(const mdraft_gdr_layer* layer, const mdraft_cache* cache, int32_t layer_index, const void* q, int64_t ldq, const void* k,
+                       int64_t ldk, const void* v, int64_t ldv, const void* z, int64_t ldz, const void* dt, int64_t lddt, const void* beta,
+                       int64_t ldbeta, void* out, int64_t ldo, int32_t total_tokens, int32_t n_seq, int32_t max_seqlen, const int32_t* cu_seqlens,
+                       const int32_t* init_slot, const int32_t* final_slot, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                       void* stream) {
+    int rc = check_gdr_layer(layer);
+    if (rc) return rc;
+    if (total_tokens < 0 || n_seq < 0 || max_seqlen < 0) return MDRAFT_ERR_INVALID_ARG;
+    if (init_slot || final_slot || cache) {
+        rc = check_states(cache, (int64_t)layer->n_v_heads * layer->d_v * layer->d_k, layer_index);
+        if (rc) return rc;
+    }
+    if (n_seq == 0) return MDRAFT_OK;
+    if (!cu_seqlens && n_seq != 1) return MDRAFT_ERR_INVALID_ARG;
+    GdrPrefillArgs a;
+    a.io = {q, k, v, z, dt, beta, out, ldq, ldk, ldv, ldz, lddt, ldbeta, ldo};
+    if ((rc = check_gdr_io(layer, a.io, total_tokens > 0))) return rc;
+    if (n_seq > 65535) return MDRAFT_ERR_UNSUPPORTED;
+    a.L = gdr_layer_dev(layer);
+    a.pool = states_dev(cache, layer_index);
+    a.T = total_tokens; a.n_seq = n_seq; a.n_chunks_bound = 0;
+    a.cu = cu_seqlens; a.init_slot = init_slot; a.final_slot = final_slot; a.dev_status = dev_status;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return launch_gdr_sequential(a, layer->d_k, layer->d_v, layer->act, st) == cudaSuccess ? MDRAFT_OK : MDRAFT_ERR_CUDA;
+}
+
+int mdraft_gdr_tree_step(const mdraft_gdr_layer* layer, const mdraft_cache* cache, int32_t layer_index, const void* q, int64_t ldq,
+                         const void* k, int64_t ldk, const void* v, int64_t ldv, const void* z, int64_t ldz, const void* dt, int64_t lddt,
+                         const void* beta, int64_t ldbeta, void* out, int64_t ldo, int32_t n_nodes, const int32_t* parent_slot,
+                         const int32_t* node_slot, int32_t n_levels, const int32_t* level_offsets, int32_t* dev_status, void* stream) {
+    int rc = check_gdr_layer(layer);
+    if (rc) return rc;
+    if ((rc = check_states(cache, (int64_t)layer->n_v_heads * layer->d_v * layer->d_k, layer_index))) return rc;
+    if (n_nodes < 0 || n_levels < 0) return MDRAFT_ERR_INVALID_ARG;
+    if (n_nodes == 0) return MDRAFT_OK;
+    if (!parent_slot || !node_slot) return MDRAFT_ERR_INVALID_ARG;
+    if (!level_offsets && n_levels > 1) return MDRAFT_ERR_INVALID_ARG;
+    if (level_offsets) {
+        if (n_levels < 1 || level_offsets[0] != 0 || level_offsets[n_levels] != n_nodes) return MDRAFT_ERR_INVALID_ARG;
+        for (int l = 0; l < n_levels; ++l)
+            if (level_offsets[l + 1] < level_offsets[l]) return MDRAFT_ERR_INVALID_ARG;
+    }
+    GdrStepArgs a;
+    a.io = {q, k, v, z, dt, beta, out, ldq, ldk, ldv, ldz, lddt, ldbeta, ldo};
+    if ((rc = check_gdr_io(layer, a.io, true))) return rc;
+    a.L = gdr_layer_dev(layer);
+    a.pool = states_dev(cache, layer_index);
+    a.parent_slot = parent_slot; a.node_slot = node_slot; a.dev_status = dev_status;
+    const int levels = level_offsets ? n_levels : 1;
+    a.level_in_call = 0;
+    for (int l = 0; l < levels; ++l) {
+        a.lvl_begin = level_offsets ? level_offsets[l] : 0;
+        a.lvl_end = level_offsets ? level_offsets[l + 1] : n_nodes;
+        if (a.lvl_end == a.lvl_begin) continue;
+        if (launch_gdr_step(a, layer->d_k, layer->d_v, layer->act, static_cast<cudaStream_t>(stream)) != cudaSuccess) return MDRAFT_ERR_CUDA;
+        ++a.level_in_call;
+    }
+    return MDRAFT_OK;
+}
+
+int mdraft_gdr_state_commit(const mdraft_cache* cache, int32_t d_inner, int32_t d_state, int32_t conv_channels, int32_t d_conv, int32_t act,
+                            int32_t n_commit, const int32_t* src_slot, const int32_t* dst_slot, int32_t* dev_status, void* stream) {
+    if (d_inner <= 0 || conv_channels < 0 || n_commit < 0) return MDRAFT_ERR_INVALID_ARG;
+    if ((d_state != 64 && d_state != 128) || d_conv != kW || conv_channels % 8 != 0 || (act != MDRAFT_F32 && act != MDRAFT_BF16)) return MDRAFT_ERR_UNSUPPORTED;
+    int rc = check_states(cache, (int64_t)d_inner * d_state, 0);
+    if (rc) return rc;
+    const int64_t es = (int64_t)elem_size(act), window = (int64_t)(kW - 1) * conv_channels;
+    if (conv_channels > 0) {
+        if (!cache->conv || cache->conv_slot_stride < window || (cache->n_layers > 1 && cache->conv_layer_stride < 0)) return MDRAFT_ERR_INVALID_ARG;
+        if (!aligned16(cache->conv) || (cache->conv_slot_stride * es) % 16 || (cache->conv_layer_stride * es) % 16) return MDRAFT_ERR_MISALIGNED;
+    }
+    if (n_commit == 0) return MDRAFT_OK;
+    if (!src_slot || !dst_slot) return MDRAFT_ERR_INVALID_ARG;
+    CommitArgs a;
+    a.ssm = reinterpret_cast<char*>(cache->ssm);
+    a.conv = static_cast<char*>(cache->conv);
+    a.ssm_layer_bytes = cache->ssm_layer_stride * 4; a.ssm_slot_bytes_stride = cache->ssm_slot_stride * 4;
+    a.conv_layer_bytes = cache->conv_layer_stride * es; a.conv_slot_bytes_stride = cache->conv_slot_stride * es;
+    a.ssm_bytes = (int64_t)d_inner * d_state * 4; a.conv_bytes = window * es;
+    a.n_layers = cache->n_layers; a.n_slots = cache->n_slots; a.dev_status = dev_status;
+    if (a.n_layers > 65535) return MDRAFT_ERR_UNSUPPORTED;
+    for (int off = 0; off < n_commit; off += 65535) {
+        a.n_commit = n_commit - off < 65535 ? n_commit - off : 65535;
+        a.src_slot = src_slot + off; a.dst_slot = dst_slot + off;
+        if (launch_commit(a, static_cast<cudaStream_t>(stream)) != cudaSuccess) return MDRAFT_ERR_CUDA;
+    }
+    return MDRAFT_OK;
+}
+
+int mdraft_qk_norm(const mdraft_qk_norm_spec* spec, const void* q, int64_t ldq, const void* k, int64_t ldk, void* q_out, int64_t ldqo,
+                   void* k_out, int64_t ldko, const int32_t* positions, int32_t n_rows, void* stream) {
+    if (!spec || spec->n_q_heads < 0 || spec->n_k_heads < 0 || spec->rot_dim < 0 || n_rows < 0) return MDRAFT_ERR_INVALID_ARG;
+    if (spec->norm < MDRAFT_NORM_NONE || spec->norm > MDRAFT_NORM_RMS || spec->rot_layout < MDRAFT_ROT_HALF || spec->rot_layout > MDRAFT_ROT_PAIRS)
+        return MDRAFT_ERR_INVALID_ARG;
+    const int d = spec->d_head, act = spec->act;
+    if (d < 8 || d > 256 || d % 8 != 0 || spec->n_q_heads > 65536 || spec->n_k_heads > 65536 || (act != MDRAFT_F32 && act != MDRAFT_BF16)) return MDRAFT_ERR_UNSUPPORTED;
+    if (spec->rot_dim > d || spec->rot_dim % (spec->rot_layout == MDRAFT_ROT_HALF ? 16 : 2) != 0) return MDRAFT_ERR_UNSUPPORTED;
+    if (spec->rot_dim > 0 && !spec->freqs) return MDRAFT_ERR_INVALID_ARG;
+    if ((spec->q_w && !aligned16(spec->q_w)) || (spec->k_w && !aligned16(spec->k_w))) return MDRAFT_ERR_MISALIGNED;
+    if (n_rows == 0 || spec->n_q_heads + spec->n_k_heads == 0) return MDRAFT_OK;
+    int rc;
+    if ((rc = check_matrix(q, ldq, spec->n_q_heads * d, act, spec->n_q_heads > 0))) return rc;
+    if ((rc = check_matrix(q_out, ldqo, spec->n_q_heads * d, act, spec->n_q_heads > 0))) return rc;
+    if ((rc = check_matrix(k, ldk, spec->n_k_heads * d, act, spec->n_k_heads > 0))) return rc;
+    if ((rc = check_matrix(k_out, ldko, spec->n_k_heads * d, act, spec->n_k_heads > 0))) return rc;
+    if (spec->rot_dim > 0 && !positions) return MDRAFT_ERR_INVALID_ARG;
+    QkNormArgs a = {q, k, q_out, k_out, ldq, ldk, ldqo, ldko, positions, spec->q_w, spec->k_w, spec->freqs, n_rows, d, spec->n_q_heads, spec->n_k_heads,
+                    spec->norm, spec->rot_dim, spec->rot_layout, spec->eps, spec->rot_scale};
+    return launch_qk_norm(a, act, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MDRAFT_OK : MDRAFT_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -1,0 +1,66 @@
+// Launch interface of the gated-delta-rule kernels (internal to the library).
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+
+namespace mdraft {
+
+constexpr int kGdrQ = 64;   // tokens per chunk of the chunked context encode
+
+// Per-layer constants as the kernels take them.
+struct GdrLayerDev {
+    const float* A;        // (Hv)
+    const float* dt_bias;  // (Hv) or NULL
+    const float* norm_w;   // (d_v) or NULL: no output norm
+    int n_k_heads, n_v_heads;
+    uint32_t flags;
+    float scale, eps;
+};
+
+// Activations of a call; rows are tokens or nodes.
+struct GdrIo {
+    const void *q, *k, *v, *z, *dt, *beta;   // z may be NULL: no gate
+    void* out;
+    int64_t ldq, ldk, ldv, ldz, lddt, ldb, ldo;
+};
+
+struct GdrPrefillArgs {
+    GdrLayerDev L;
+    PoolDev pool;              // slot = (Hv * d_v, d_k) fp32
+    GdrIo io;
+    int T, n_seq, n_chunks_bound;
+    const int32_t *cu, *init_slot, *final_slot;
+    int32_t* dev_status;
+};
+
+// Token by token: one kernel, no workspace.
+cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int act, cudaStream_t st);
+
+struct GdrStepArgs {
+    GdrLayerDev L;
+    PoolDev pool;
+    GdrIo io;
+    const int32_t *parent_slot, *node_slot;
+    int level_in_call;   // kernels this call has launched before this level
+    int lvl_begin, lvl_end;
+    int32_t* dev_status;
+};
+
+cudaError_t launch_gdr_step(const GdrStepArgs& p, int d_k, int d_v, int act, cudaStream_t st);
+
+// ---------------------------------------------------------------- device helpers shared by the kernels
+// Decay and write strength of one token and head: alpha = exp(Delta A), beta (MDRAFT_BETA_SIGMOID: of its pre-activation).
+template <typename T>
+__device__ __forceinline__ float gdr_log2_decay(const GdrLayerDev& L, const T* dt, int head) {
+    const float v = Act<T>::to_f32(*dt) + (L.dt_bias ? __ldg(L.dt_bias + head) : 0.f);
+    return ((L.flags & MDRAFT_DT_SOFTPLUS) ? softplus(v) : v) * __ldg(L.A + head) * kLog2e;
+}
+template <typename T>
+__device__ __forceinline__ float gdr_beta(const GdrLayerDev& L, const T* b) {
+    const float v = Act<T>::to_f32(*b);
+    return (L.flags & MDRAFT_BETA_SIGMOID) ? rcp(1.0f + ex2(-kLog2e * v)) : v;
+}
+
+}  // namespace mdraft

@@ -29,6 +29,10 @@ struct Entry {
     decltype(&mdraft_conv_scan_prefill_stack) prefill_stack;
     decltype(&mdraft_tree_step_stack) tree_step_stack;
     decltype(&mdraft_block_generation) block_generation;
+    decltype(&mdraft_gdr_prefill) gdr_prefill;
+    decltype(&mdraft_gdr_tree_step) gdr_tree_step;
+    decltype(&mdraft_gdr_state_commit) gdr_commit;
+    decltype(&mdraft_qk_norm) qk_norm;
 };
 
 struct Failed {};  // a Python exception is set
@@ -40,7 +44,8 @@ struct Failed {};  // a Python exception is set
 
 // Attribute names, interned once.
 struct Names {
-    PyObject *A, *D, *conv_w, *conv_b, *dt_bias, *act, *flags, *d_inner, *d_state, *d_conv, *headdim, *ssm, *conv, *n_layers, *n_slots, *cuda_stream, *cuda_event;
+    PyObject *A, *D, *conv_w, *conv_b, *dt_bias, *act, *flags, *d_inner, *d_state, *d_conv, *headdim, *ssm, *conv, *n_layers, *n_slots, *cuda_stream, *cuda_event,
+        *n_k_heads, *n_v_heads, *d_k, *d_v, *scale, *eps, *norm_w, *conv_channels, *d_head, *n_q_heads, *norm, *rot_dim, *rot_layout, *rot_scale, *q_w, *k_w, *freqs;
 };
 Names N;
 
@@ -550,10 +555,164 @@ PyObject* block_generation(PyObject* const* a) {
     });
 }
 
+// ---------------------------------------------------------------- delta layer
+float attr_float(PyObject* owner, PyObject* name) {
+    Ref r(PyObject_GetAttr(owner, name));
+    const double v = PyFloat_AsDouble(r.p);
+    if (v == -1.0 && PyErr_Occurred()) throw Failed();
+    return (float)v;
+}
+
+void on_current_device(const at::Tensor& t, const char* name) {
+    if (!t.is_cuda() || t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, std::string(name) + ": must be a CUDA tensor of the current device");
+}
+
+// Rows of `cols` activations; None = absent, where that is allowed.  `rows` < 0: any number.
+Matrix activations(PyObject* o, const char* name, int act, int64_t cols, int64_t rows, bool optional = false) {
+    if (o == Py_None && !optional) fail(PyExc_TypeError, std::string(name) + ": must be a tensor");
+    Matrix m(Py_None, name);
+    if (o == Py_None) return m;
+    const at::Tensor& t = tensor(o, name);
+    if (t.dim() == 2 && t.size(0) == 0) { m.p = t.const_data_ptr(); m.ld = cols; }   // strides of nothing mean nothing
+    else m = Matrix(o, name);
+    if (m.rows == 1) m.ld = cols;   // nor does the step to a second row that is not there
+    on_current_device(t, name);
+    if (t.scalar_type() != (act == MDRAFT_BF16 ? at::kBFloat16 : at::kFloat)) fail(PyExc_TypeError, std::string(name) + ": must have the layer's activation dtype");
+    if (t.size(1) != cols || (rows >= 0 && t.size(0) != rows))
+        fail(PyExc_ValueError, std::string(name) + ": need " + (rows >= 0 ? std::to_string(rows) + " x " : std::string("rows of ")) + std::to_string(cols) + " values");
+    return m;
+}
+
+// Contiguous int32 indices of the current device; None = absent.
+const int32_t* device_indices(PyObject* o, int64_t n, const char* name) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != at::kInt) fail(PyExc_TypeError, std::string(name) + " must be int32");
+    on_current_device(t, name);
+    if ((n >= 0 && t.numel() != n) || !t.is_contiguous()) fail(PyExc_ValueError, std::string(name) + ": need " + std::to_string(n) + " contiguous entries");
+    return static_cast<const int32_t*>(t.const_data_ptr());
+}
+
+int32_t* status_word(PyObject* o) {
+    if (o != Py_None && (tensor(o, "dev_status").scalar_type() != at::kInt || tensor(o, "dev_status").numel() < 1)) fail(PyExc_TypeError, "dev_status must be int32");
+    if (o != Py_None) on_current_device(tensor(o, "dev_status"), "dev_status");
+    return static_cast<int32_t*>(mutable_data(o, "dev_status"));
+}
+
+mdraft_gdr_layer gdr_layer_of(PyObject* o, PyObject* flags) {
+    mdraft_gdr_layer l;
+    l.n_k_heads = (int32_t)attr_int(o, N.n_k_heads); l.n_v_heads = (int32_t)attr_int(o, N.n_v_heads);
+    l.d_k = (int32_t)attr_int(o, N.d_k); l.d_v = (int32_t)attr_int(o, N.d_v);
+    l.act = act_of(o);
+    l.flags = (uint32_t)(flags == Py_None ? attr_int(o, N.flags) : as_int(flags));
+    l.scale = attr_float(o, N.scale); l.eps = attr_float(o, N.eps);
+    l.A = static_cast<const float*>(attr_data(o, N.A)); l.dt_bias = static_cast<const float*>(attr_data(o, N.dt_bias));
+    l.norm_w = static_cast<const float*>(attr_data(o, N.norm_w));
+    return l;
+}
+
+// A pool of delta-layer states: fp32, as wide as the layer, dense slots, on the current device.
+struct States : Cache {
+    States(PyObject* o, const mdraft_gdr_layer& l) : Cache(o) {
+        if (!present) return;
+        Ref s(PyObject_GetAttr(o, N.ssm));
+        const at::Tensor& t = tensor(s.p, "ssm");
+        on_current_device(t, "the cache");
+        if (t.scalar_type() != at::kFloat || t.dim() != 4 || t.size(2) != (int64_t)l.n_v_heads * l.d_v || t.size(3) != l.d_k || t.stride(3) != 1 || t.stride(2) != l.d_k)
+            fail(PyExc_ValueError, "the cache's slots must be fp32 states of n_v_heads * d_v rows of d_k values");
+    }
+};
+
+// The eight activations of a delta-layer call.
+struct GdrTensors {
+    Matrix v, q, k, z, dt, beta, out;
+    int64_t rows;
+    GdrTensors(PyObject* const* a, const mdraft_gdr_layer& l)
+        : v(activations(a[2], "v", l.act, (int64_t)l.n_v_heads * l.d_v, -1)),
+          q(activations(a[0], "q", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)), k(activations(a[1], "k", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)),
+          z(activations(a[3], "z", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows, true)), dt(activations(a[4], "dt", l.act, l.n_v_heads, v.rows)),
+          beta(activations(a[5], "beta", l.act, l.n_v_heads, v.rows)), out(activations(a[6], "out", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows)), rows(v.rows) {}
+};
+
+// (table, layer, cache, layer_index, q, k, v, z, dt, beta, out, cu_seqlens, max_seqlen, init_slot, final_slot, workspace, dev_status,
+//  stream, flags)
+PyObject* gdr_prefill(PyObject* const* a) {
+    const mdraft_gdr_layer l = gdr_layer_of(a[1], a[18]);
+    const States c(a[2], l);
+    const int32_t li = (int32_t)as_int(a[3]), longest = (int32_t)as_int(a[12]);
+    const GdrTensors t(a + 4, l);
+    const int32_t* cu = device_indices(a[11], -1, "cu_seqlens");
+    const int64_t n_seq = cu ? tensor(a[11], "cu_seqlens").numel() - 1 : 1;
+    const int32_t *init = device_indices(a[13], n_seq, "init_slot"), *fin = device_indices(a[14], n_seq, "final_slot");
+    const Workspace ws(a[15]);
+    if (ws.p) on_current_device(tensor(a[15], "workspace"), "workspace");
+    int32_t* st = status_word(a[16]);
+    void* stream = stream_of(a[17]);
+    const Entry& e = entry(a[0]);
+    return released([&] {
+        return e.gdr_prefill(&l, c.get(), li, t.q.p, t.q.ld, t.k.p, t.k.ld, t.v.p, t.v.ld, t.z.p, t.z.ld, t.dt.p, t.dt.ld, t.beta.p, t.beta.ld, t.out.out(),
+                             t.out.ld, (int32_t)t.rows, (int32_t)n_seq, longest, cu, init, fin, ws.p, ws.bytes, st, stream);
+    });
+}
+
+// (table, layer, cache, layer_index, q, k, v, z, dt, beta, out, parent_slot, node_slot, level_offsets, dev_status, stream, flags)
+PyObject* gdr_tree_step(PyObject* const* a) {
+    const mdraft_gdr_layer l = gdr_layer_of(a[1], a[16]);
+    const States c(a[2], l);
+    const int32_t li = (int32_t)as_int(a[3]);
+    const GdrTensors t(a + 4, l);
+    const int32_t *parent = device_indices(a[11], t.rows, "parent_slot"), *node = device_indices(a[12], t.rows, "node_slot");
+    const Levels lv(a[13]);
+    int32_t* st = status_word(a[14]);
+    void* stream = stream_of(a[15]);
+    const Entry& e = entry(a[0]);
+    return released([&] {
+        return e.gdr_tree_step(&l, c.get(), li, t.q.p, t.q.ld, t.k.p, t.k.ld, t.v.p, t.v.ld, t.z.p, t.z.ld, t.dt.p, t.dt.ld, t.beta.p, t.beta.ld, t.out.out(),
+                               t.out.ld, (int32_t)t.rows, parent, node, lv.count(), lv.get(), st, stream);
+    });
+}
+
+// (table, cache, src_slot, dst_slot, dev_status, stream)
+PyObject* gdr_commit(PyObject* const* a) {
+    const Cache c(a[1]);
+    if (!c.present) fail(PyExc_TypeError, "cache must not be None");
+    const int32_t d = (int32_t)attr_int(a[1], N.d_inner), n = (int32_t)attr_int(a[1], N.d_state), w = (int32_t)attr_int(a[1], N.d_conv);
+    const int32_t channels = (int32_t)attr_int(a[1], N.conv_channels);
+    const int act = act_of(a[1]);
+    const int64_t m = tensor(a[2], "src_slot").numel();
+    const int32_t *src = device_indices(a[2], m, "src_slot"), *dst = device_indices(a[3], m, "dst_slot");
+    int32_t* st = status_word(a[4]);
+    void* stream = stream_of(a[5]);
+    const Entry& e = entry(a[0]);
+    return released([&] { return e.gdr_commit(c.get(), d, n, channels, w, act, (int32_t)m, src, dst, st, stream); });
+}
+
+// (table, spec, q, k, q_out, k_out, positions, stream)
+PyObject* qk_norm(PyObject* const* a) {
+    mdraft_qk_norm_spec s;
+    PyObject* o = a[1];
+    s.d_head = (int32_t)attr_int(o, N.d_head); s.n_q_heads = (int32_t)attr_int(o, N.n_q_heads); s.n_k_heads = (int32_t)attr_int(o, N.n_k_heads);
+    s.act = act_of(o);
+    s.norm = (int32_t)attr_int(o, N.norm); s.rot_dim = (int32_t)attr_int(o, N.rot_dim); s.rot_layout = (int32_t)attr_int(o, N.rot_layout);
+    s.eps = attr_float(o, N.eps); s.rot_scale = attr_float(o, N.rot_scale);
+    s.q_w = static_cast<const float*>(attr_data(o, N.q_w)); s.k_w = static_cast<const float*>(attr_data(o, N.k_w));
+    s.freqs = static_cast<const float*>(attr_data(o, N.freqs));
+    const int64_t qc = (int64_t)s.n_q_heads * s.d_head, kc = (int64_t)s.n_k_heads * s.d_head;
+    const bool no_q = s.n_q_heads == 0, no_k = s.n_k_heads == 0;
+    const Matrix q(activations(a[2], "q", s.act, qc, -1, no_q)), k(activations(a[3], "k", s.act, kc, no_q ? -1 : q.rows, no_k));
+    const int64_t rows = no_q ? k.rows : q.rows;
+    const Matrix qo(activations(a[4], "q_out", s.act, qc, rows, no_q)), ko(activations(a[5], "k_out", s.act, kc, rows, no_k));
+    const int32_t* pos = device_indices(a[6], rows, "positions");
+    void* stream = stream_of(a[7]);
+    const Entry& e = entry(a[0]);
+    return released([&] { return e.qk_norm(&s, q.p, q.ld, k.p, k.ld, qo.out(), qo.ld, ko.out(), ko.ld, pos, (int32_t)rows, stream); });
+}
+
 #define ENTRY(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(table, 1), ENTRY(prefill, 20), ENTRY(prefill_noalloc, 18), ENTRY(tree_step, 16), ENTRY(tree_step_proj, 15),
                          ENTRY(commit, 6), ENTRY(ssd_prefill, 17), ENTRY(ssd_tree_step, 16), ENTRY(prefill_stack, 13),
-                         ENTRY(tree_step_stack, 11), ENTRY(block_generation, 15), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(tree_step_stack, 11), ENTRY(block_generation, 15), ENTRY(gdr_prefill, 19), ENTRY(gdr_tree_step, 17),
+                         ENTRY(gdr_commit, 6), ENTRY(qk_norm, 8), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_host", "argument marshalling for libmdraft.so", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -563,7 +722,10 @@ PyMODINIT_FUNC PyInit__host() {
     struct { PyObject** to; const char* text; } all[] = {
         {&N.A, "A"}, {&N.D, "D"}, {&N.conv_w, "conv_w"}, {&N.conv_b, "conv_b"}, {&N.dt_bias, "dt_bias"}, {&N.act, "act"}, {&N.flags, "flags"},
         {&N.d_inner, "d_inner"}, {&N.d_state, "d_state"}, {&N.d_conv, "d_conv"}, {&N.headdim, "headdim"}, {&N.ssm, "ssm"}, {&N.conv, "conv"},
-        {&N.n_layers, "n_layers"}, {&N.n_slots, "n_slots"}, {&N.cuda_stream, "cuda_stream"}, {&N.cuda_event, "cuda_event"}};
+        {&N.n_layers, "n_layers"}, {&N.n_slots, "n_slots"}, {&N.cuda_stream, "cuda_stream"}, {&N.cuda_event, "cuda_event"},
+        {&N.n_k_heads, "n_k_heads"}, {&N.n_v_heads, "n_v_heads"}, {&N.d_k, "d_k"}, {&N.d_v, "d_v"}, {&N.scale, "scale"}, {&N.eps, "eps"},
+        {&N.norm_w, "norm_w"}, {&N.conv_channels, "conv_channels"}, {&N.d_head, "d_head"}, {&N.n_q_heads, "n_q_heads"}, {&N.norm, "norm"},
+        {&N.rot_dim, "rot_dim"}, {&N.rot_layout, "rot_layout"}, {&N.rot_scale, "rot_scale"}, {&N.q_w, "q_w"}, {&N.k_w, "k_w"}, {&N.freqs, "freqs"}};
     for (auto& n : all)
         if (!(*n.to = PyUnicode_InternFromString(n.text))) return nullptr;
     return PyModule_Create(&module_def);
