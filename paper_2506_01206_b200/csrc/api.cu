@@ -1028,6 +1028,42 @@ GdrLayerDev gdr_layer_dev(const mdraft_gdr_layer* L) {
     return d;
 }
 
+// How an encode is done: token by token, or in chunks.
+struct GdrPlan {
+    bool chunked;
+    int n_chunks_bound, slice;
+    size_t off_M, off_csl, off_o, bytes;
+};
+
+constexpr int kGdrSequentialMax = 32;   // tokens
+
+GdrPlan plan_gdr(const mdraft_gdr_layer* L, int T, int n_seq, int max_seqlen) {
+    GdrPlan pl = {};
+    if (max_seqlen > T) max_seqlen = T;
+    pl.chunked = L->act == MDRAFT_BF16 && max_seqlen > kGdrSequentialMax;
+    if (!pl.chunked) return pl;
+    pl.n_chunks_bound = n_seq + T / kGdrQ;
+    const size_t n = (size_t)pl.n_chunks_bound * L->n_v_heads;
+    pl.slice = (int64_t)n_seq * L->n_v_heads * (L->d_v / 16) <= sm_count() ? 16 : 32;
+    pl.off_M = align_up(n * kGdrTBytes, 256);
+    pl.off_csl = align_up(pl.off_M + n * kGdrMBytes, 256);
+    pl.off_o = align_up(pl.off_csl + n * kGdrQ * sizeof(float2), 256);
+    pl.bytes = align_up(pl.off_o + (L->norm_w ? (size_t)T * L->n_v_heads * L->d_v * sizeof(float) : 0), 256);
+    return pl;
+}
+
+// Descriptor of a (rows x cols) row-major bf16 matrix read in boxes of box_cols x 64 rows.
+bool encode_gdr_matrix(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_cols, bool swizzled) {
+    PFN_cuTensorMapEncodeTiled enc = tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t gstride[1] = {(cuuint64_t)ld * 2};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)kGdrQ};
+    cuuint32_t estride[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 PoolDev states_dev(const mdraft_cache* c, int layer_index) {
     PoolDev p = {};
     if (!c) return p;
@@ -1042,7 +1078,8 @@ PoolDev states_dev(const mdraft_cache* c, int layer_index) {
 extern "C" {
 
 size_t mdraft_gdr_prefill_workspace_bytes(const mdraft_gdr_layer* layer, int32_t total_tokens, int32_t n_seq, int32_t max_seqlen) {
-    return 0;
+    if (check_gdr_layer(layer) != MDRAFT_OK || total_tokens <= 0 || n_seq <= 0 || max_seqlen < 0) return 0;
+    return plan_gdr(layer, total_tokens, n_seq, max_seqlen).bytes;
 }
 
 int mdraft_gdr_prefill(const mdraft_gdr_layer* layer, const mdraft_cache* cache, int32_t layer_index, const void* q, int64_t ldq, const void* k,
@@ -1068,6 +1105,20 @@ int mdraft_gdr_prefill(const mdraft_gdr_layer* layer, const mdraft_cache* cache,
     a.T = total_tokens; a.n_seq = n_seq; a.n_chunks_bound = 0;
     a.cu = cu_seqlens; a.init_slot = init_slot; a.final_slot = final_slot; a.dev_status = dev_status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const GdrPlan pl = plan_gdr(layer, total_tokens, n_seq, max_seqlen);
+    if (pl.chunked) {
+        if (!workspace || workspace_bytes < pl.bytes) return MDRAFT_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MDRAFT_ERR_MISALIGNED;
+        a.n_chunks_bound = pl.n_chunks_bound;
+        unsigned char* w = static_cast<unsigned char*>(workspace);
+        const GdrChunkWs ws = {w, w + pl.off_M, reinterpret_cast<float2*>(w + pl.off_csl), layer->norm_w ? reinterpret_cast<float*>(w + pl.off_o) : nullptr};
+        GdrMaps maps;
+        const int64_t kc = (int64_t)layer->n_k_heads * layer->d_k, vc = (int64_t)layer->n_v_heads * layer->d_v;
+        if (!encode_gdr_matrix(&maps.q, q, total_tokens, kc, ldq, 64, true) || !encode_gdr_matrix(&maps.k, k, total_tokens, kc, ldk, 64, true) ||
+            !encode_gdr_matrix(&maps.v, v, total_tokens, vc, ldv, pl.slice, false))
+            return MDRAFT_ERR_CUDA;
+        return launch_gdr_chunked(a, ws, maps, layer->d_k, layer->d_v, pl.slice, st) == cudaSuccess ? MDRAFT_OK : MDRAFT_ERR_CUDA;
+    }
     return launch_gdr_sequential(a, layer->d_k, layer->d_v, layer->act, st) == cudaSuccess ? MDRAFT_OK : MDRAFT_ERR_CUDA;
 }
 

@@ -38,6 +38,23 @@ struct GdrPrefillArgs {
 // Token by token: one kernel, no workspace.
 cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int act, cudaStream_t st);
 
+// Scratch of the chunked encode, per (chunk, value head).
+constexpr uint32_t kGdrTBytes = 15360, kGdrMBytes = 5120;   // lower triangles in 16 x 16 blocks, as the chain's lanes hold them
+struct GdrChunkWs {
+    unsigned char* T;   // (1 + A)^-1 diag(beta), split into three bf16 values
+    unsigned char* M;   // masked products of queries and keys, bf16
+    float2* csl;        // 64 running log2 decays (value, remainder)
+    float* o;           // (T, Hv * d_v) fp32 outputs before the norm; NULL: there is no norm
+};
+
+// TMA descriptors of one call: boxes of 64 values x 64 rows of q and k, of a slice x 64 rows of v.
+struct GdrMaps {
+    CUtensorMap q, k, v;
+};
+
+// Chunks side by side, then a chain over the chunks of each sequence; `slice` = values of a head per block of the chain (16 or 32).
+cudaError_t launch_gdr_chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_k, int d_v, int slice, cudaStream_t st);
+
 struct GdrStepArgs {
     GdrLayerDev L;
     PoolDev pool;

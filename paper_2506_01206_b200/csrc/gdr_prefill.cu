@@ -1,0 +1,639 @@
+// Chunked context encode of the gated delta rule (bf16 activations).
+//
+// Over a chunk of Q = 64 tokens, with G_i the running log decay, the recurrence is a triangular system: token i writes
+//
+//     x_i = beta_i (v_i - e^{G_i} S k_i - sum_{j<i} e^{G_i - G_j} (k_i . k_j) x_j)          S: the chunk's incoming state
+//
+// so with A_ij = beta_i e^{G_i - G_j} k_i . k_j (j < i) and T = (1 + A)^-1 diag(beta), per value head:
+//
+//     X  = T (V - e^G (K S^T))                                     what the chunk's tokens write
+//     O  = scale (e^G (Q S^T) + (Q K^T o e^{G_i - G_j})_{j <= i} X)
+//     S' = e^{G_end} S + (e^{G_end - G} X)^T K
+//
+// T and the masked products M = scale (Q K^T o e^{..}) need the chunk alone: kernel 1 forms them for all chunks side by side.  What is left is a
+// chain over the chunks of a sequence, kernel 2, whose rows of S (values) are independent: a block takes a slice of them.
+//
+//   1. gdr_chunk_prepare, a block per (value head, chunk): [K; Q] K^T as one product of 128 rows on the tensor cores (tcgen05, operands by
+//      TMA), then the triangle's inverse by forward substitution in fp32, a column per thread.  Results go to the workspace in
+//      the order in which kernel 2's lanes hold them.
+//   2. gdr_chain, a block per (slice of d_v, value head, sequence): state in registers, three small products per chunk one after another
+//      (K S^T; T times the difference; the update), beside them the two of the outputs.
+//   3. gdr_norm_gate where there is an output norm, which needs all slices of a row.
+//
+// Precision.  States keep fp32 accuracy: q, k, v are bf16 as given; everything else that meets them in a product of the state's path (S, T, the
+// differences, X) is split into three bf16 values (24 bits), which costs three products with an exact operand and six where both are
+// split.  Two values (16 bits) left an error of 3e-6 in the states.  The outputs' products take S and M as one bf16 value and X as two.
+//
+// Kernel 2 runs on the warp-level tensor instructions (mma.sync), not on tcgen05: its products are 64 x 16 x 128 and depend on
+// one another, so what counts is the way from one to the next (registers to shared memory and back, a barrier) and not the rate.
+#include "chunk_map.cuh"
+#include "common.cuh"
+#include "gdr.cuh"
+#include "tensor_core.cuh"
+
+namespace mdraft {
+
+namespace {
+
+constexpr int Q = kGdrQ;
+constexpr int kBlocks = 10;                            // 16 x 16 blocks of a lower triangle of 64 x 64
+constexpr uint32_t kTBytes = kGdrTBytes, kMBytes = kGdrMBytes;
+static_assert(kTBytes == 3 * kBlocks * 512 && kMBytes == kBlocks * 512, "workspace layout");
+
+// ---------------------------------------------------------------- kernel 1
+constexpr int kPrepThreads = 128;
+constexpr int kPitch = 68;   // floats of a row of A and M
+
+template <int DK>
+struct PrepSmem {
+    static constexpr int kTile = DK / 64 * 128 * 128 > Q * kPitch * 4 ? DK / 64 * 128 * 128 : Q * kPitch * 4;
+    unsigned char kq[kTile];       // [K; Q] rows in boxes of 64 values, 128-byte swizzle  ->  M as fp32
+    float A[Q][kPitch];            // A, then T
+    float2 csl[Q];                 // running log2 decay (value, remainder)
+    float beta[Q];
+    double warp_sum;
+    uint64_t bar_tma, bar_mma;
+    uint32_t tmem_base;
+};
+
+// 16 bytes of a lane's share of a 16 x 16 block at (row0, col0) of a fp32 matrix as the A operand of a warp's product: pairs of neighbouring columns.
+__device__ __forceinline__ void operand_pairs(const float (*m)[kPitch], int row0, int col0, int lane, float2 (&v)[4]) {
+    const int g = lane >> 2, t = 2 * (lane & 3);
+    v[0] = *reinterpret_cast<const float2*>(&m[row0 + g][col0 + t]);
+    v[1] = *reinterpret_cast<const float2*>(&m[row0 + g + 8][col0 + t]);
+    v[2] = *reinterpret_cast<const float2*>(&m[row0 + g][col0 + t + 8]);
+    v[3] = *reinterpret_cast<const float2*>(&m[row0 + g + 8][col0 + t + 8]);
+}
+
+// What the state decays by from one token to another, log2.
+__device__ __forceinline__ float log2_between(float2 from, float2 to) { return (to.x - from.x) + (to.y - from.y); }
+
+// x as three bf16 values, two neighbours at a time.
+__device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+    hi = pack_bf(a, b);
+    a -= bf_lo(hi); b -= bf_hi(hi);
+    mid = pack_bf(a, b);
+    lo = pack_bf(a - bf_lo(mid), b - bf_hi(mid));
+}
+
+template <int DK>
+__global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps) {
+    extern __shared__ __align__(1024) unsigned char s_raw[];
+    PrepSmem<DK>& sm = *reinterpret_cast<PrepSmem<DK>*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int head = blockIdx.x, cidx = blockIdx.y + blockIdx.z * gridDim.y;
+    grid_wait();
+    grid_release_dependents();
+    const ChunkInfo ci = find_chunk(p.cu, p.n_seq, p.T, Q, p.n_chunks_bound, cidx);
+    if (ci.seq < 0) return;
+    const int rows = ci.t1 - ci.t0;
+    const int kcol = head / (p.L.n_v_heads / p.L.n_k_heads) * DK;
+    if (tid == 0) {
+        mbar_init(&sm.bar_tma, 1);
+        mbar_init(&sm.bar_mma, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        mbar_expect_tx(&sm.bar_tma, DK / 64 * 128 * 128);
+#pragma unroll
+        for (int h = 0; h < DK / 64; ++h) {
+            tma_box(sm.kq + h * 16384, &maps.k, kcol + 64 * h, ci.t0, &sm.bar_tma);
+            tma_box(sm.kq + h * 16384 + 8192, &maps.q, kcol + 64 * h, ci.t0, &sm.bar_tma);
+        }
+    }
+    if (warp == 0) { tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
+    float g = 0.f, beta = 0.f;   // rows past the chunk's end: no decay, nothing written
+    if (tid < rows) {
+        const size_t t = (size_t)(ci.t0 + tid);
+        g = gdr_log2_decay(p.L, static_cast<const __nv_bfloat16*>(p.io.dt) + t * p.io.lddt + head, head);
+        beta = gdr_beta(p.L, static_cast<const __nv_bfloat16*>(p.io.beta) + t * p.io.ldb + head);
+    }
+    // Running sums in 64 bits, kept as two fp32 values: what is wanted is their differences, and a head that forgets at once sums to 10^4.
+    double sum = g;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+    }
+    if (tid == 31) sm.warp_sum = sum;
+    __syncthreads();
+    tc_fence_after();
+    if (tid < Q) {
+        if (warp == 1) sum += sm.warp_sum;
+        const float hi = (float)sum;
+        sm.csl[tid] = make_float2(hi, (float)(sum - hi));
+        sm.beta[tid] = beta;
+        ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = sm.csl[tid];
+    }
+    const uint32_t tmem = sm.tmem_base;
+    const bool in_ok = mbar_wait_bounded(&sm.bar_tma, 0u);
+    if (in_ok && tid == 0) {
+        tc_fence_after();
+        const uint64_t d = operand_desc_sw128(smem_u32(sm.kq));
+#pragma unroll
+        for (int k = 0; k < DK / 16; ++k) {   // rows: keys and queries; columns: keys
+            const uint64_t at = d + (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4);
+            mma_bf16(tmem, at, at, instr_desc(Q, false, false), k > 0);
+        }
+        mma_commit(&sm.bar_mma);
+    }
+    bool ok = in_ok && mbar_wait_bounded(&sm.bar_mma, 0u);
+    ok = !__syncthreads_or(!ok);   // csl and beta are visible, the operands are free
+    if (ok) {
+        tc_fence_after();
+        const bool query = warp >= 2;
+        const int i = tid & 63;
+        float* row = query ? reinterpret_cast<float(*)[kPitch]>(sm.kq)[i] : sm.A[i];
+        const float2 mine = sm.csl[i];
+        const float f = i < rows ? (query ? p.L.scale : sm.beta[i]) : 0.f;
+        const int last = i < rows ? (query ? i : i - 1) : -1;   // columns up to here count
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[32];
+            tmem_ld32(tmem + ((uint32_t)(warp * 32) << 16) + h * 32, v);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                float4 w;
+                float* e = &w.x;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = h * 32 + j + u;
+                    e[u] = c <= last ? v[j + u] * f * ex2(log2_between(sm.csl[c], mine)) : 0.f;   // replaced, not scaled: what is masked may be anything
+                }
+                *reinterpret_cast<float4*>(row + h * 32 + j) = w;
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 0) tmem_free(tmem, 64);
+    if (!ok) {
+        if (tid == 0) {
+            flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
+            if (!in_ok) mbar_wait_bounded(&sm.bar_tma, 0u);   // the copies target this block's shared memory: one more bounded chance
+        }
+        return;
+    }
+    // (1 + A)^-1 diag(beta), column tid: x_i = e_i - sum_{j<i} A_ij x_j
+    float x[Q];
+    if (tid < Q) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            float a = 0.f, b = 0.f, c = 0.f, d = 0.f;
+#pragma unroll
+            for (int j = 0; j + 3 < i; j += 4) {
+                const float4 r = *reinterpret_cast<const float4*>(&sm.A[i][j]);
+                a = fmaf(r.x, x[j], a); b = fmaf(r.y, x[j + 1], b); c = fmaf(r.z, x[j + 2], c); d = fmaf(r.w, x[j + 3], d);
+            }
+#pragma unroll
+            for (int j = i & ~3; j < i; ++j) a = fmaf(sm.A[i][j], x[j], a);
+            x[i] = (i == tid ? 1.f : 0.f) - ((a + b) + (c + d));
+        }
+    }
+    __syncthreads();
+    if (tid < Q) {
+        const float b = sm.beta[tid];
+#pragma unroll
+        for (int i = 0; i < Q; ++i) sm.A[i][tid] = i >= tid ? x[i] * b : 0.f;
+    }
+    __syncthreads();
+    const float (*M)[kPitch] = reinterpret_cast<const float (*)[kPitch]>(sm.kq);
+    unsigned char* to_T = ws.T + ((size_t)cidx * p.L.n_v_heads + head) * kTBytes + lane * 16;
+    unsigned char* to_M = ws.M + ((size_t)cidx * p.L.n_v_heads + head) * kMBytes + lane * 16;
+    for (int n = warp; n < kBlocks; n += kPrepThreads / 32) {
+        const int mi = n < 1 ? 0 : (n < 3 ? 1 : (n < 6 ? 2 : 3)), ki = n - mi * (mi + 1) / 2;
+        float2 v[4];
+        operand_pairs(sm.A, mi * 16, ki * 16, lane, v);
+        uint32_t s[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split3(v[e].x, v[e].y, s[0][e], s[1][e], s[2][e]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + (k * kBlocks + n) * 512) = make_uint4(s[k][0], s[k][1], s[k][2], s[k][3]);
+        operand_pairs(M, mi * 16, ki * 16, lane, v);
+        *reinterpret_cast<uint4*>(to_M + n * 512) =
+            make_uint4(pack_bf(v[0].x, v[0].y), pack_bf(v[1].x, v[1].y), pack_bf(v[2].x, v[2].y), pack_bf(v[3].x, v[3].y));
+    }
+}
+
+// ---------------------------------------------------------------- kernel 2
+constexpr int kChainThreads = 512;   // warps 0-7: the state's products; warps 8-15: the outputs'
+
+template <int DK, int DVS>
+struct ChainStage {
+    unsigned char k[Q * DK * 2], q[Q * DK * 2];   // boxes of 64 values x 64 rows, 128-byte swizzle
+    unsigned char T[kTBytes], M[kMBytes];
+    __nv_bfloat16 v[Q][DVS];
+    float2 csl[Q];
+    unsigned char pad[1024 - (kTBytes + kMBytes + Q * DVS * 2 + Q * 8) % 1024];
+};
+template <int DK, int DVS, int STAGES>
+struct ChainSmem {
+    static constexpr int kRow = DVS + 8;                // values of a row of the operands below, padded against bank conflicts
+    ChainStage<DK, DVS> stage[STAGES];
+    __nv_bfloat16 S[3][DVS][DK];                        // state split in three, 16-byte units XOR-ed with the row index
+    __nv_bfloat16 R[3][Q][kRow];                        // beta^-1 of what is written, split in three
+    __nv_bfloat16 W[3][Q][kRow];                        // e^{G_end - G} X, split in three
+    __nv_bfloat16 X[2][Q][kRow];                        // X, split in two
+    uint64_t full[STAGES];
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm2t(uint32_t (&r)[2], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void lds16(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+template <int DK, int DVS, int STAGES>
+__global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps, int d_v) {
+    using Smem = ChainSmem<DK, DVS, STAGES>;
+    constexpr int kRow = Smem::kRow;
+    constexpr int NT = DVS / 16;        // 8-column tiles of a warp in products of 64 x DVS
+    constexpr int MS = DVS / 16;        // 16-row tiles of the state slice
+    constexpr int ND = DK / 64;         // 8-column tiles of a warp in the state slice
+    extern __shared__ __align__(1024) unsigned char s_raw[];
+    Smem& sm = *reinterpret_cast<Smem*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, w8 = warp & 7;
+    const bool outputs = warp >= 8;
+    const int slice = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+    grid_release_dependents();
+    int first, nck, s0, len;
+    bool bad;
+    seq_chunks(p.cu, p.n_seq, p.T, Q, p.n_chunks_bound, seq, first, nck);
+    seq_span(p.cu, p.n_seq, p.T, seq, s0, len, bad);
+    const int islot = load_slot(p.init_slot, seq), fslot = load_slot(p.final_slot, seq);
+    const bool bad_slot = islot >= p.pool.n_slots || fslot >= p.pool.n_slots;
+    if (bad || bad_slot || (len > 0 && nck == 0)) {   // malformed offsets, chunks beyond the workspace, slots that are not there: left out
+        if (tid == 0 && slice == 0 && head == 0) flag(p.dev_status, bad_slot ? MDRAFT_DEV_BAD_SLOT : MDRAFT_DEV_BAD_SEQLENS);
+        grid_wait();
+        return;
+    }
+    const int khead = head / (p.L.n_v_heads / p.L.n_k_heads), col = head * d_v + slice * DVS;
+    const size_t H = p.L.n_v_heads;
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) mbar_init(&sm.full[i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    grid_wait();   // T, M and the running decays are the work of the kernel just before
+    __syncthreads();
+    auto fetch = [&](int c, int st) {   // one thread
+        ChainStage<DK, DVS>& s = sm.stage[st];
+        const int t0 = s0 + c * Q;
+        const size_t ch = (size_t)(first + c) * H + head;
+        mbar_expect_tx(&sm.full[st], 2 * Q * DK * 2 + kTBytes + kMBytes + Q * DVS * 2 + Q * 8);
+#pragma unroll
+        for (int h = 0; h < DK / 64; ++h) {
+            tma_box(s.k + h * 8192, &maps.k, khead * DK + 64 * h, t0, &sm.full[st]);
+            tma_box(s.q + h * 8192, &maps.q, khead * DK + 64 * h, t0, &sm.full[st]);
+        }
+        tma_box(s.v, &maps.v, col, t0, &sm.full[st]);
+        bulk_load(s.T, ws.T + ch * kTBytes, kTBytes, &sm.full[st]);
+        bulk_load(s.M, ws.M + ch * kMBytes, kMBytes, &sm.full[st]);
+        bulk_load(s.csl, ws.csl + ch * Q, Q * 8, &sm.full[st]);
+    };
+    if (tid == kChainThreads - 32)
+        for (int i = 0; i < STAGES && i < nck; ++i) fetch(i, i);
+
+    // The warp's tile of a 64 x DVS product: rows 16 mt .., column tiles n0 ..; the triangles' work is even over the schedulers (warps w and w + 4).
+    const int mt = w8 < 4 ? w8 : 7 - w8, n0 = (w8 >> 2) * NT;
+    const int g = lane >> 2, t2 = 2 * (lane & 3);
+    const int r0 = mt * 16 + g, r1 = r0 + 8;
+    const uint32_t sS = smem_u32(sm.S), sR = smem_u32(sm.R), sW = smem_u32(sm.W), sX = smem_u32(sm.X);
+    // State: rows (values) 16 ms + g and + 8, columns 8 (w8 ND + nd) + t2 and + 1.
+    float S[MS][ND][4];
+    if (!outputs) {
+        const float* h0 = p.pool.ssm + (size_t)(islot < 0 ? 0 : islot) * p.pool.ssm_slot_stride + (size_t)col * DK;
+#pragma unroll
+        for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+            for (int nd = 0; nd < ND; ++nd) {
+                float2 a = make_float2(0.f, 0.f), b = a;
+                const int c = (w8 * ND + nd) * 8 + t2;
+                if (islot >= 0) {
+                    a = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g) * DK + c);
+                    b = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g + 8) * DK + c);
+                }
+                S[ms][nd][0] = a.x; S[ms][nd][1] = a.y; S[ms][nd][2] = b.x; S[ms][nd][3] = b.y;
+            }
+    }
+    auto store_split_state = [&] {
+#pragma unroll
+        for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+            for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = ms * 16 + g + 8 * h, unit = w8 * ND + nd;
+                    uint32_t s[3];
+                    split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], s[0], s[1], s[2]);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[k][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = s[k];
+                }
+    };
+    if (!outputs) store_split_state();
+    __syncthreads();
+
+    for (int c = 0; c < nck; ++c) {
+        const int st = c % STAGES;
+        ChainStage<DK, DVS>& s = sm.stage[st];
+        const int t0 = s0 + c * Q, rows = min(Q, len - c * Q);
+        const bool here = mbar_wait_bounded(&sm.full[st], (uint32_t)(c / STAGES) & 1u);
+        if (rows < Q) {   // rows of other sequences, which may hold anything, meet zeros in products over the tokens: they have to be zeros too
+            for (int i = tid; i < (Q - rows) * (DK / 8); i += kChainThreads) {
+                const int r = rows + i / (DK / 8), u = i % (DK / 8);
+                *reinterpret_cast<uint4*>(s.k + (u >> 3) * 8192 + r * 128 + (u & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            __syncthreads();
+        }
+        const float2 end = s.csl[Q - 1];
+        const uint32_t sA = smem_u32(outputs ? s.q : s.k);
+        const int arow = mt * 16 + (lane & 15);
+        float acc[3][NT][4];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[k][n][e] = 0.f;
+        // K S^T, or Q S^T with the state's leading part
+#pragma unroll
+        for (int k2 = 0; k2 < DK / 32; ++k2) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int ks = 2 * k2 + h, unit = (ks & 3) * 2 + (lane >> 4);
+                ldsm4(a[h], sA + (ks >> 2) * 8192 + arow * 128 + ((unit ^ (arow & 7)) * 16));
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                if (k > 0 && outputs) break;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t b[4];
+                    const int row = (n0 + n) * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
+                    ldsm4(b, sS + (k * DVS + row) * (DK * 2) + ((unit ^ (row & 7)) * 16));
+                    mma16816(acc[k][n], a[0], b[0], b[1]);
+                    mma16816(acc[k][n], a[1], b[2], b[3]);
+                }
+            }
+        }
+        const float e0 = ex2(s.csl[r0].x), e1 = ex2(s.csl[r1].x);
+        uint32_t zr[NT][2];
+        if (!outputs) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int cc = (n0 + n) * 8 + t2;
+                const uint32_t v0 = *reinterpret_cast<const uint32_t*>(&s.v[r0][cc]), v1 = *reinterpret_cast<const uint32_t*>(&s.v[r1][cc]);
+                float d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = (acc[2][n][e] + acc[1][n][e]) + acc[0][n][e];
+                d[0] = r0 < rows ? fmaf(-e0, d[0], bf_lo(v0)) : 0.f;
+                d[1] = r0 < rows ? fmaf(-e0, d[1], bf_hi(v0)) : 0.f;
+                d[2] = r1 < rows ? fmaf(-e1, d[2], bf_lo(v1)) : 0.f;
+                d[3] = r1 < rows ? fmaf(-e1, d[3], bf_hi(v1)) : 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[3];
+                    split3(d[2 * h], d[2 * h + 1], x[0], x[1], x[2]);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.R[k][r0 + 8 * h][cc]) = x[k];
+                }
+            }
+            bar_sync(1, 256);
+            // X = T R: blocks of T up to the diagonal, the six products that reach 24 bits
+            float x0[NT][4], x1[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { x0[n][e] = 0.f; x1[n][e] = 0.f; }
+            const uint32_t sT = smem_u32(s.T) + (mt * (mt + 1) / 2) * 512 + lane * 16;
+            for (int ki = 0; ki <= mt; ++ki) {
+                uint32_t a[3][4];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) lds16(a[k], sT + (k * kBlocks + ki) * 512);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t b[3][2];
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) ldsm2t(b[k], sR + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
+                    mma16816(x0[n], a[0], b[0][0], b[0][1]);
+                    mma16816(x1[n], a[0], b[2][0], b[2][1]);
+                    mma16816(x0[n], a[0], b[1][0], b[1][1]);
+                    mma16816(x1[n], a[2], b[0][0], b[0][1]);
+                    mma16816(x0[n], a[1], b[0][0], b[0][1]);
+                    mma16816(x1[n], a[1], b[1][0], b[1][1]);
+                }
+            }
+            const float f0 = ex2(log2_between(s.csl[r0], end)), f1 = ex2(log2_between(s.csl[r1], end));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int cc = (n0 + n) * 8 + t2;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float a = x0[n][2 * h] + x1[n][2 * h], b = x0[n][2 * h + 1] + x1[n][2 * h + 1], f = h ? f1 : f0;
+                    uint32_t w[3], x[3];
+                    split3(a * f, b * f, w[0], w[1], w[2]);
+                    split3(a, b, x[0], x[1], x[2]);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.W[k][r0 + 8 * h][cc]) = w[k];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) *reinterpret_cast<uint32_t*>(&sm.X[k][r0 + 8 * h][cc]) = x[k];
+                }
+            }
+        } else if (p.io.z && !ws.o) {
+            const __nv_bfloat16* z = static_cast<const __nv_bfloat16*>(p.io.z) + (size_t)(t0 + r0) * p.io.ldz + col;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                zr[n][0] = zr[n][1] = 0u;
+                if (r0 < rows) zr[n][0] = *reinterpret_cast<const uint32_t*>(z + (n0 + n) * 8 + t2);
+                if (r1 < rows) zr[n][1] = *reinterpret_cast<const uint32_t*>(z + 8 * p.io.ldz + (n0 + n) * 8 + t2);
+            }
+        }
+        __syncthreads();   // W and X are there; the state's operands have been read
+        if (!outputs) {
+            const float ec = ex2(end.x);
+            float m[MS][ND][4];
+#pragma unroll
+            for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { S[ms][nd][e] *= ec; m[ms][nd][e] = 0.f; }
+#pragma unroll
+            for (int ki = 0; ki < Q / 16; ++ki) {
+                uint32_t b[4];
+                const int row = ki * 16 + (lane & 15);
+                if (ND == 2) {
+                    const int unit = (w8 & 3) * 2 + (lane >> 4);
+                    ldsm4t(b, sA + (w8 >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
+                } else {
+                    uint32_t b2[2];
+                    ldsm2t(b2, sA + row * 128 + ((w8 ^ (row & 7)) * 16));
+                    b[0] = b2[0]; b[1] = b2[1]; b[2] = b[3] = 0u;
+                }
+#pragma unroll
+                for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        uint32_t a[4];
+                        ldsm4t(a, sW + ((k * Q + ki * 16 + (lane & 7) + ((lane >> 4) & 1) * 8) * kRow + ms * 16 + ((lane >> 3) & 1) * 8) * 2);
+#pragma unroll
+                        for (int nd = 0; nd < ND; ++nd) mma16816(k == 0 ? S[ms][nd] : m[ms][nd], a, b[2 * nd], b[2 * nd + 1]);
+                    }
+            }
+#pragma unroll
+            for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[ms][nd][e] += m[ms][nd][e];
+            store_split_state();
+        } else {
+            // O = scale e^G (Q S^T) + M X
+            float o[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                o[n][0] = acc[0][n][0] * (e0 * p.L.scale); o[n][1] = acc[0][n][1] * (e0 * p.L.scale);
+                o[n][2] = acc[0][n][2] * (e1 * p.L.scale); o[n][3] = acc[0][n][3] * (e1 * p.L.scale);
+            }
+            const uint32_t sM = smem_u32(s.M) + (mt * (mt + 1) / 2) * 512 + lane * 16;
+            for (int ki = 0; ki <= mt; ++ki) {
+                uint32_t a[4];
+                lds16(a, sM + ki * 512);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t b[2];
+                        ldsm2t(b, sX + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
+                        mma16816(o[n], a, b[0], b[1]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = r0 + 8 * h;
+                    if (r >= rows) continue;
+                    const size_t t = (size_t)(t0 + r);
+                    const int cc = col + (n0 + n) * 8 + t2;
+                    float a = o[n][2 * h], b = o[n][2 * h + 1];
+                    if (ws.o) {
+                        *reinterpret_cast<float2*>(ws.o + t * (H * d_v) + cc) = make_float2(a, b);
+                    } else {
+                        if (p.io.z) { a *= silu(bf_lo(zr[n][h])); b *= silu(bf_hi(zr[n][h])); }
+                        *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.io.out) + t * p.io.ldo + cc) = pack_bf(a, b);
+                    }
+                }
+        }
+        // the state's operands are there, the stage is free
+        if (__syncthreads_or(!here)) {   // a copy did not arrive in time
+            if (tid == 0) {
+                flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
+                for (int i = c; i < c + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
+            }
+            __syncthreads();
+            return;
+        }
+        if (tid == kChainThreads - 32 && c + STAGES < nck) fetch(c + STAGES, st);
+    }
+    if (!outputs && fslot >= 0 && (nck > 0 || fslot != islot)) {
+        float* h1 = p.pool.ssm + (size_t)fslot * p.pool.ssm_slot_stride + (size_t)col * DK;
+#pragma unroll
+        for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+            for (int nd = 0; nd < ND; ++nd) {
+                const int c = (w8 * ND + nd) * 8 + t2;
+                *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g) * DK + c) = make_float2(S[ms][nd][0], S[ms][nd][1]);
+                *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g + 8) * DK + c) = make_float2(S[ms][nd][2], S[ms][nd][3]);
+            }
+    }
+}
+
+// ---------------------------------------------------------------- kernel 3: output norm and gate, a warp per row and head
+constexpr int kNormThreads = 256;
+
+template <int DV>
+__global__ void __launch_bounds__(kNormThreads) gdr_norm_gate(const GdrPrefillArgs p, const float* o) {
+    constexpr int E = DV / 32;   // values of a lane
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = p.L.n_v_heads;
+    grid_wait();
+    grid_release_dependents();
+    const ChunkInfo ci = find_chunk(p.cu, p.n_seq, p.T, Q, p.n_chunks_bound, blockIdx.y + blockIdx.z * gridDim.y);
+    if (ci.seq < 0 || load_slot(p.init_slot, ci.seq) >= p.pool.n_slots || load_slot(p.final_slot, ci.seq) >= p.pool.n_slots) return;
+    const int head = blockIdx.x;
+    float w[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = __ldg(p.L.norm_w + lane * E + e);
+#pragma unroll 4
+    for (int t = ci.t0 + warp; t < ci.t1; t += kNormThreads / 32) {
+        const size_t c = (size_t)head * DV + lane * E;
+        float v[E], z[E], sq = 0.f;
+        uint32_t zr[E / 2];
+        if (E == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(o + (size_t)t * H * DV + c);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(o + (size_t)t * H * DV + c);
+        if (p.io.z) {
+            const __nv_bfloat16* zp = static_cast<const __nv_bfloat16*>(p.io.z) + (size_t)t * p.io.ldz + c;
+            if (E == 4) *reinterpret_cast<uint2*>(zr) = *reinterpret_cast<const uint2*>(zp);
+            else zr[0] = *reinterpret_cast<const uint32_t*>(zp);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) sq = fmaf(v[e], v[e], sq);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+        const float f = rsqrtf(sq * (1.0f / DV) + p.L.eps);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            z[e] = p.io.z ? silu(e & 1 ? bf_hi(zr[e / 2]) : bf_lo(zr[e / 2])) : 1.f;
+            v[e] *= f * w[e] * z[e];
+        }
+        __nv_bfloat16* op = static_cast<__nv_bfloat16*>(p.io.out) + (size_t)t * p.io.ldo + c;
+        if (E == 4) *reinterpret_cast<uint2*>(op) = make_uint2(pack_bf(v[0], v[1]), pack_bf(v[2], v[3]));
+        else *reinterpret_cast<uint32_t*>(op) = pack_bf(v[0], v[1]);
+    }
+}
+
+// Blocks over (heads, chunks) where there may be more chunks than a grid's second index takes.
+inline dim3 chunk_grid(int heads, int chunks) {
+    const int z = (chunks + 65534) / 65535;
+    return dim3(heads, (chunks + z - 1) / z, z);
+}
+
+template <int DK, int DVS, int STAGES>
+cudaError_t chain(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_v, cudaStream_t st) {
+    constexpr int smem = sizeof(ChainSmem<DK, DVS, STAGES>) + 1024;
+    static_assert(smem <= 227 * 1024, "one block per SM");
+    const cudaError_t e = allow_smem<gdr_chain<DK, DVS, STAGES>>(smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(gdr_chain<DK, DVS, STAGES>, dim3(d_v / DVS, p.L.n_v_heads, p.n_seq), kChainThreads, smem, st, p, ws, maps, d_v);
+}
+
+template <int DK>
+cudaError_t chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_v, int slice, cudaStream_t st) {
+    constexpr int smem = sizeof(PrepSmem<DK>) + 1024;
+    cudaError_t e = allow_smem<gdr_chunk_prepare<DK>>(smem);
+    if (e != cudaSuccess) return e;
+    if ((e = launch_pdl(gdr_chunk_prepare<DK>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kPrepThreads, smem, st, p, ws, maps)) != cudaSuccess) return e;
+    e = slice == 16 ? chain<DK, 16, 3>(p, ws, maps, d_v, st) : chain<DK, 32, 2>(p, ws, maps, d_v, st);
+    if (e != cudaSuccess || !ws.o) return e;
+    return launch_pdl(d_v == 128 ? gdr_norm_gate<128> : gdr_norm_gate<64>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kNormThreads, 0, st, p, ws.o);
+}
+
+}  // namespace
+
+cudaError_t launch_gdr_chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_k, int d_v, int slice, cudaStream_t st) {
+    return d_k == 128 ? chunked<128>(p, ws, maps, d_v, slice, st) : chunked<64>(p, ws, maps, d_v, slice, st);
+}
+
+}  // namespace mdraft
