@@ -48,8 +48,11 @@ template <int DK>
 struct PrepSmem {
     static constexpr int kTile = DK / 64 * 128 * 128 > Q * kPitch * 4 ? DK / 64 * 128 * 128 : Q * kPitch * 4;
     unsigned char kq[kTile];       // [K; Q] rows in boxes of 64 values, 128-byte swizzle  ->  M as fp32
-    float A[Q][kPitch];            // A, then T
+    float A[Q][kPitch];            // blocks of A, each replaced by its block of the inverse
+    float Z[32][36];               // product on the way to a block of the inverse
     float2 csl[Q];                 // running log2 decay (value, remainder)
+    float u[Q];                    // decay from the first row of a row's block to the row
+    float v[4][Q];                 // decay from a row to the first row of a later block
     float beta[Q];
     double warp_sum;
     uint64_t bar_tma, bar_mma;
@@ -74,6 +77,27 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
     a -= bf_lo(hi); b -= bf_hi(hi);
     mid = pack_bf(a, b);
     lo = pack_bf(a - bf_lo(mid), b - bf_hi(mid));
+}
+
+// Four neighbouring columns of a row times a matrix: sum over k < K of a[k] b[k][0..3], b's rows `pitch` floats apart.
+template <int K>
+__device__ __forceinline__ float4 small_product(const float* a, const float* b, int pitch) {
+    u64 lo = 0ull, hi = 0ull;
+#pragma unroll
+    for (int k = 0; k < K; k += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(a + k);
+        const float e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(b + (k + i) * pitch);
+            lo = fma2(pk(e[i], e[i]), y.x, lo);
+            hi = fma2(pk(e[i], e[i]), y.y, hi);
+        }
+    }
+    float4 r;
+    unpk(lo, r.x, r.y);
+    unpk(hi, r.z, r.w);
+    return r;
 }
 
 template <int DK>
@@ -123,6 +147,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         sm.beta[tid] = beta;
         ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = sm.csl[tid];
     }
+    __syncthreads();
     const uint32_t tmem = sm.tmem_base;
     const bool in_ok = mbar_wait_bounded(&sm.bar_tma, 0u);
     if (in_ok && tid == 0) {
@@ -135,30 +160,42 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         }
         mma_commit(&sm.bar_mma);
     }
+    // Decays between rows of different 16 x 16 blocks in two factors, both at most 1, by way of the first row of the later block.
+    if (tid < Q) sm.u[tid] = ex2(log2_between(sm.csl[tid & ~15], sm.csl[tid]));
+    for (int i = tid; i < 96; i += kPrepThreads) {
+        const int blk = i < 16 ? 1 : (i < 48 ? 2 : 3), j = i - (blk == 1 ? 0 : (blk == 2 ? 16 : 48));
+        sm.v[blk][j] = ex2(log2_between(sm.csl[j], sm.csl[16 * blk]));
+    }
     bool ok = in_ok && mbar_wait_bounded(&sm.bar_mma, 0u);
-    ok = !__syncthreads_or(!ok);   // csl and beta are visible, the operands are free
+    ok = !__syncthreads_or(!ok);   // the decays are visible, the operands are free
     if (ok) {
         tc_fence_after();
         const bool query = warp >= 2;
-        const int i = tid & 63;
+        const int i = tid & 63, rb = i >> 4;
         float* row = query ? reinterpret_cast<float(*)[kPitch]>(sm.kq)[i] : sm.A[i];
         const float2 mine = sm.csl[i];
-        const float f = i < rows ? (query ? p.L.scale : sm.beta[i]) : 0.f;
+        const float f = i < rows ? (query ? p.L.scale : sm.beta[i]) : 0.f, fu = f * sm.u[i];
         const int last = i < rows ? (query ? i : i - 1) : -1;   // columns up to here count
+        for (int cb = 0; cb < 2 + 2 * (warp & 1); ++cb) {       // blocks that some row of the warp has
+            float v[16];
+            __syncwarp();
+            tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + cb * 16, v);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[32];
-            tmem_ld32(tmem + ((uint32_t)(warp * 32) << 16) + h * 32, v);
+            for (int j = 0; j < 16; j += 4) {
+                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (cb < rb) {
+                    const float4 d = *reinterpret_cast<const float4*>(&sm.v[rb][cb * 16 + j]);
+                    w = make_float4(v[j] * (fu * d.x), v[j + 1] * (fu * d.y), v[j + 2] * (fu * d.z), v[j + 3] * (fu * d.w));
+                    if (i >= rows) w = make_float4(0.f, 0.f, 0.f, 0.f);
+                } else if (cb == rb) {
+                    float* e = &w.x;
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                float4 w;
-                float* e = &w.x;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int c = h * 32 + j + u;
-                    e[u] = c <= last ? v[j + u] * f * ex2(log2_between(sm.csl[c], mine)) : 0.f;   // replaced, not scaled: what is masked may be anything
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = cb * 16 + j + k;
+                        e[k] = c <= last ? v[j + k] * f * ex2(log2_between(sm.csl[c], mine)) : 0.f;   // replaced, not scaled: what is masked may be anything
+                    }
                 }
-                *reinterpret_cast<float4*>(row + h * 32 + j) = w;
+                *reinterpret_cast<float4*>(row + cb * 16 + j) = w;
             }
         }
         tc_fence_before();
@@ -172,27 +209,49 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         }
         return;
     }
-    // (1 + A)^-1 diag(beta), column tid: x_i = e_i - sum_{j<i} A_ij x_j
-    float x[Q];
-    if (tid < Q) {
+    // (1 + A)^-1 in place, by blocks.  Diagonal blocks of 16: a warp each, a column per lane, x_i = e_i - sum_{j<i} A_ij x_j.
+    if (lane < 16) {
+        const int o = 16 * warp;
+        float x[16];
 #pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            float a = 0.f, b = 0.f, c = 0.f, d = 0.f;
+        for (int i = 0; i < 16; ++i) {
+            float a = 0.f, b = 0.f;
 #pragma unroll
-            for (int j = 0; j + 3 < i; j += 4) {
-                const float4 r = *reinterpret_cast<const float4*>(&sm.A[i][j]);
-                a = fmaf(r.x, x[j], a); b = fmaf(r.y, x[j + 1], b); c = fmaf(r.z, x[j + 2], c); d = fmaf(r.w, x[j + 3], d);
+            for (int j = 0; j < i; j += 4) {
+                const float4 r = *reinterpret_cast<const float4*>(&sm.A[o + i][o + j]);   // zero from the diagonal on
+                a = fmaf(r.x, x[j], a);
+                if (j + 1 < i) b = fmaf(r.y, x[j + 1], b);
+                if (j + 2 < i) a = fmaf(r.z, x[j + 2], a);
+                if (j + 3 < i) b = fmaf(r.w, x[j + 3], b);
             }
-#pragma unroll
-            for (int j = i & ~3; j < i; ++j) a = fmaf(sm.A[i][j], x[j], a);
-            x[i] = (i == tid ? 1.f : 0.f) - ((a + b) + (c + d));
+            x[i] = (i == lane ? 1.f : 0.f) - (a + b);
         }
+        __syncwarp(0xffffu);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sm.A[o + i][o + lane] = x[i];
     }
     __syncthreads();
-    if (tid < Q) {
-        const float b = sm.beta[tid];
-#pragma unroll
-        for (int i = 0; i < Q; ++i) sm.A[i][tid] = i >= tid ? x[i] * b : 0.f;
+    // Blocks (1, 0) and (3, 2): -T_11 (A_10 T_00); 64 threads each, four columns of a row per thread.
+    {
+        const int o = (tid >> 6) * 32, r = (tid & 63) >> 2, c = (tid & 3) * 4;
+        float4 z = small_product<16>(&sm.A[o + 16 + r][o], &sm.A[o][o + c], kPitch);
+        *reinterpret_cast<float4*>(&sm.Z[(tid >> 6) * 16 + r][c]) = z;
+        __syncthreads();
+        z = small_product<16>(&sm.A[o + 16 + r][o + 16], &sm.Z[(tid >> 6) * 16][c], 36);
+        *reinterpret_cast<float4*>(&sm.A[o + 16 + r][o + c]) = make_float4(-z.x, -z.y, -z.z, -z.w);
+    }
+    __syncthreads();
+    // The lower left 32 x 32 likewise, rows r and r + 16.
+    {
+        const int r = tid >> 3, c = (tid & 7) * 4;
+        float4 z0 = small_product<32>(&sm.A[32 + r][0], &sm.A[0][c], kPitch), z1 = small_product<32>(&sm.A[48 + r][0], &sm.A[0][c], kPitch);
+        *reinterpret_cast<float4*>(&sm.Z[r][c]) = z0;
+        *reinterpret_cast<float4*>(&sm.Z[16 + r][c]) = z1;
+        __syncthreads();
+        z0 = small_product<16>(&sm.A[32 + r][32], &sm.Z[0][c], 36);   // the upper rows of T_11 end with its first block
+        z1 = small_product<32>(&sm.A[48 + r][32], &sm.Z[0][c], 36);
+        *reinterpret_cast<float4*>(&sm.A[32 + r][c]) = make_float4(-z0.x, -z0.y, -z0.z, -z0.w);
+        *reinterpret_cast<float4*>(&sm.A[48 + r][c]) = make_float4(-z1.x, -z1.y, -z1.z, -z1.w);
     }
     __syncthreads();
     const float (*M)[kPitch] = reinterpret_cast<const float (*)[kPitch]>(sm.kq);
@@ -202,9 +261,10 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         const int mi = n < 1 ? 0 : (n < 3 ? 1 : (n < 6 ? 2 : 3)), ki = n - mi * (mi + 1) / 2;
         float2 v[4];
         operand_pairs(sm.A, mi * 16, ki * 16, lane, v);
+        const float2 b0 = *reinterpret_cast<const float2*>(&sm.beta[ki * 16 + 2 * (lane & 3)]), b1 = *reinterpret_cast<const float2*>(&sm.beta[ki * 16 + 2 * (lane & 3) + 8]);
         uint32_t s[3][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) split3(v[e].x, v[e].y, s[0][e], s[1][e], s[2][e]);
+        for (int e = 0; e < 4; ++e) split3(v[e].x * (e < 2 ? b0.x : b1.x), v[e].y * (e < 2 ? b0.y : b1.y), s[0][e], s[1][e], s[2][e]);
 #pragma unroll
         for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + (k * kBlocks + n) * 512) = make_uint4(s[k][0], s[k][1], s[k][2], s[k][3]);
         operand_pairs(M, mi * 16, ki * 16, lane, v);
@@ -214,7 +274,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
 }
 
 // ---------------------------------------------------------------- kernel 2
-constexpr int kChainThreads = 512;   // warps 0-7: the state's products; warps 8-15: the outputs'
+constexpr int kChainThreads = 384;   // warps 0-7: the state's products; warps 8-11: the outputs'
 
 template <int DK, int DVS>
 struct ChainStage {
@@ -253,16 +313,20 @@ __device__ __forceinline__ void lds16(uint32_t (&r)[4], uint32_t a) {
 }
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
+// The state's warps load what does not depend on the product ahead of it before the barrier in between: the next chunk's key rows, the rows of T,
+// the key columns of the update.  (With every operand loaded behind its barrier a chunk of 128 x 128 took 4100 cycles instead of ???.)
 template <int DK, int DVS, int STAGES>
 __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps, int d_v) {
     using Smem = ChainSmem<DK, DVS, STAGES>;
     constexpr int kRow = Smem::kRow;
-    constexpr int NT = DVS / 16;        // 8-column tiles of a warp in products of 64 x DVS
+    constexpr int NT = DVS / 16;        // 8-column tiles of a state warp in products of 64 x DVS
+    constexpr int NQ = DVS / 8;         // and of an output warp
     constexpr int MS = DVS / 16;        // 16-row tiles of the state slice
     constexpr int ND = DK / 64;         // 8-column tiles of a warp in the state slice
+    constexpr int KS = DK / 16;         // steps over d_k
     extern __shared__ __align__(1024) unsigned char s_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, w8 = warp & 7;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool outputs = warp >= 8;
     const int slice = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
     grid_release_dependents();
@@ -304,104 +368,119 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
     if (tid == kChainThreads - 32)
         for (int i = 0; i < STAGES && i < nck; ++i) fetch(i, i);
 
-    // The warp's tile of a 64 x DVS product: rows 16 mt .., column tiles n0 ..; the triangles' work is even over the schedulers (warps w and w + 4).
-    const int mt = w8 < 4 ? w8 : 7 - w8, n0 = (w8 >> 2) * NT;
     const int g = lane >> 2, t2 = 2 * (lane & 3);
-    const int r0 = mt * 16 + g, r1 = r0 + 8;
     const uint32_t sS = smem_u32(sm.S), sR = smem_u32(sm.R), sW = smem_u32(sm.W), sX = smem_u32(sm.X);
-    // State: rows (values) 16 ms + g and + 8, columns 8 (w8 ND + nd) + t2 and + 1.
-    float S[MS][ND][4];
-    if (!outputs) {
-        const float* h0 = p.pool.ssm + (size_t)(islot < 0 ? 0 : islot) * p.pool.ssm_slot_stride + (size_t)col * DK;
-#pragma unroll
-        for (int ms = 0; ms < MS; ++ms)
-#pragma unroll
-            for (int nd = 0; nd < ND; ++nd) {
-                float2 a = make_float2(0.f, 0.f), b = a;
-                const int c = (w8 * ND + nd) * 8 + t2;
-                if (islot >= 0) {
-                    a = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g) * DK + c);
-                    b = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g + 8) * DK + c);
-                }
-                S[ms][nd][0] = a.x; S[ms][nd][1] = a.y; S[ms][nd][2] = b.x; S[ms][nd][3] = b.y;
-            }
-    }
-    auto store_split_state = [&] {
-#pragma unroll
-        for (int ms = 0; ms < MS; ++ms)
-#pragma unroll
-            for (int nd = 0; nd < ND; ++nd)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = ms * 16 + g + 8 * h, unit = w8 * ND + nd;
-                    uint32_t s[3];
-                    split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], s[0], s[1], s[2]);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[k][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = s[k];
-                }
+    // Row tile and column tiles of the warp in products of 64 x DVS; the triangles' work is even over the schedulers (warps w and w + 4).
+    const int mt = outputs ? warp - 8 : (warp < 4 ? warp : 7 - warp), n0 = outputs ? 0 : (warp >> 2) * NT;
+    const int r0 = mt * 16 + g, r1 = r0 + 8;
+    // Operand of 16 rows of keys or queries, step ks of d_k.
+    auto rows_operand = [&](uint32_t (&a)[4], const unsigned char* m, int ks) {
+        const int row = mt * 16 + (lane & 15), unit = (ks & 3) * 2 + (lane >> 4);
+        ldsm4(a, smem_u32(m) + (ks >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
     };
-    if (!outputs) store_split_state();
-    __syncthreads();
+    // Operand of 8 values of the state, steps 2 k2 and 2 k2 + 1 of d_k.
+    auto state_operand = [&](uint32_t (&b)[4], int part, int n, int k2) {
+        const int row = n * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
+        ldsm4(b, sS + (part * DVS + row) * (DK * 2) + ((unit ^ (row & 7)) * 16));
+    };
+    bool here = true, failed = false;
+    int c = 0;
+    auto arrive = [&](int n) { here = mbar_wait_bounded(&sm.full[n % STAGES], (uint32_t)(n / STAGES) & 1u) && here; };
 
-    for (int c = 0; c < nck; ++c) {
-        const int st = c % STAGES;
-        ChainStage<DK, DVS>& s = sm.stage[st];
-        const int t0 = s0 + c * Q, rows = min(Q, len - c * Q);
-        const bool here = mbar_wait_bounded(&sm.full[st], (uint32_t)(c / STAGES) & 1u);
-        if (rows < Q) {   // rows of other sequences, which may hold anything, meet zeros in products over the tokens: they have to be zeros too
-            for (int i = tid; i < (Q - rows) * (DK / 8); i += kChainThreads) {
-                const int r = rows + i / (DK / 8), u = i % (DK / 8);
-                *reinterpret_cast<uint4*>(s.k + (u >> 3) * 8192 + r * 128 + (u & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            __syncthreads();
-        }
-        const float2 end = s.csl[Q - 1];
-        const uint32_t sA = smem_u32(outputs ? s.q : s.k);
-        const int arow = mt * 16 + (lane & 15);
-        float acc[3][NT][4];
+    if (!outputs) {
+        // State: rows (values) 16 ms + g and + 8, columns 8 (ND warp + nd) + t2 and + 1.
+        float S[MS][ND][4];
+        {
+            const float* h0 = p.pool.ssm + (size_t)(islot < 0 ? 0 : islot) * p.pool.ssm_slot_stride + (size_t)col * DK;
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+            for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[k][n][e] = 0.f;
-        // K S^T, or Q S^T with the state's leading part
-#pragma unroll
-        for (int k2 = 0; k2 < DK / 32; ++k2) {
-            uint32_t a[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int ks = 2 * k2 + h, unit = (ks & 3) * 2 + (lane >> 4);
-                ldsm4(a[h], sA + (ks >> 2) * 8192 + arow * 128 + ((unit ^ (arow & 7)) * 16));
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                if (k > 0 && outputs) break;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t b[4];
-                    const int row = (n0 + n) * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
-                    ldsm4(b, sS + (k * DVS + row) * (DK * 2) + ((unit ^ (row & 7)) * 16));
-                    mma16816(acc[k][n], a[0], b[0], b[1]);
-                    mma16816(acc[k][n], a[1], b[2], b[3]);
+                for (int nd = 0; nd < ND; ++nd) {
+                    float2 a = make_float2(0.f, 0.f), b = a;
+                    const int c = (warp * ND + nd) * 8 + t2;
+                    if (islot >= 0) {
+                        a = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g) * DK + c);
+                        b = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g + 8) * DK + c);
+                    }
+                    S[ms][nd][0] = a.x; S[ms][nd][1] = a.y; S[ms][nd][2] = b.x; S[ms][nd][3] = b.y;
                 }
-            }
         }
-        const float e0 = ex2(s.csl[r0].x), e1 = ex2(s.csl[r1].x);
-        uint32_t zr[NT][2];
-        if (!outputs) {
+        auto store_split_state = [&] {
+#pragma unroll
+            for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                for (int nd = 0; nd < ND; ++nd)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = ms * 16 + g + 8 * h, unit = warp * ND + nd;
+                        uint32_t s[3];
+                        split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], s[0], s[1], s[2]);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k)
+                            *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[k][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = s[k];
+                    }
+        };
+        store_split_state();
+        uint32_t kr[KS][4];        // key rows of the chunk
+        uint32_t vr[NT][2];        // values
+        float e0 = 0.f, e1 = 0.f, f0 = 0.f, f1 = 0.f, ec = 0.f;
+        auto preload = [&](int c) {
+            const ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) rows_operand(kr[ks], s.k, ks);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                vr[n][0] = *reinterpret_cast<const uint32_t*>(&s.v[r0][(n0 + n) * 8 + t2]);
+                vr[n][1] = *reinterpret_cast<const uint32_t*>(&s.v[r1][(n0 + n) * 8 + t2]);
+            }
+            const float2 end = s.csl[Q - 1], c0 = s.csl[r0], c1 = s.csl[r1];
+            e0 = ex2(c0.x); e1 = ex2(c1.x); ec = ex2(end.x);
+            f0 = ex2(log2_between(c0, end)); f1 = ex2(log2_between(c1, end));
+        };
+        if (nck > 0) {
+            arrive(0);
+            preload(0);
+        }
+        __syncthreads();
+        for (; c < nck; ++c) {
+            ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+            const int rows = len - c * Q;
+            // K S^T, a product per part of the state
+            float acc[3][NT][4];
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[k][n][e] = 0.f;
+#pragma unroll
+            for (int k2 = 0; k2 < KS / 2; ++k2)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t b[4];
+                        state_operand(b, k, n0 + n, k2);
+                        mma16816(acc[k][n], kr[2 * k2], b[0], b[1]);
+                        mma16816(acc[k][n], kr[2 * k2 + 1], b[2], b[3]);
+                    }
+            uint32_t tr[4][3][4];   // rows of T, blocks up to the diagonal (what lies behind is not used)
+            const uint32_t sT = smem_u32(s.T) + (mt * (mt + 1) / 2) * 512 + lane * 16;
+#pragma unroll
+            for (int ki = 0; ki < 4; ++ki)
+                if (ki <= mt)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) lds16(tr[ki][k], sT + (k * kBlocks + ki) * 512);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int cc = (n0 + n) * 8 + t2;
-                const uint32_t v0 = *reinterpret_cast<const uint32_t*>(&s.v[r0][cc]), v1 = *reinterpret_cast<const uint32_t*>(&s.v[r1][cc]);
                 float d[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) d[e] = (acc[2][n][e] + acc[1][n][e]) + acc[0][n][e];
-                d[0] = r0 < rows ? fmaf(-e0, d[0], bf_lo(v0)) : 0.f;
-                d[1] = r0 < rows ? fmaf(-e0, d[1], bf_hi(v0)) : 0.f;
-                d[2] = r1 < rows ? fmaf(-e1, d[2], bf_lo(v1)) : 0.f;
-                d[3] = r1 < rows ? fmaf(-e1, d[3], bf_hi(v1)) : 0.f;
+                d[0] = r0 < rows ? fmaf(-e0, d[0], bf_lo(vr[n][0])) : 0.f;
+                d[1] = r0 < rows ? fmaf(-e0, d[1], bf_hi(vr[n][0])) : 0.f;
+                d[2] = r1 < rows ? fmaf(-e1, d[2], bf_lo(vr[n][1])) : 0.f;
+                d[3] = r1 < rows ? fmaf(-e1, d[3], bf_hi(vr[n][1])) : 0.f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[3];
@@ -411,58 +490,65 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 }
             }
             bar_sync(1, 256);
-            // X = T R: blocks of T up to the diagonal, the six products that reach 24 bits
-            float x0[NT][4], x1[NT][4];
+            // X = T R, the six products that reach 24 bits
+            float x0[NT][4], x1[NT][4], x2[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { x0[n][e] = 0.f; x1[n][e] = 0.f; }
-            const uint32_t sT = smem_u32(s.T) + (mt * (mt + 1) / 2) * 512 + lane * 16;
-            for (int ki = 0; ki <= mt; ++ki) {
-                uint32_t a[3][4];
+                for (int e = 0; e < 4; ++e) x0[n][e] = x1[n][e] = x2[n][e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 3; ++k) lds16(a[k], sT + (k * kBlocks + ki) * 512);
+            for (int ki = 0; ki < 4; ++ki)
+                if (ki <= mt) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t b[3][2];
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t b[3][2];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) ldsm2t(b[k], sR + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
-                    mma16816(x0[n], a[0], b[0][0], b[0][1]);
-                    mma16816(x1[n], a[0], b[2][0], b[2][1]);
-                    mma16816(x0[n], a[0], b[1][0], b[1][1]);
-                    mma16816(x1[n], a[2], b[0][0], b[0][1]);
-                    mma16816(x0[n], a[1], b[0][0], b[0][1]);
-                    mma16816(x1[n], a[1], b[1][0], b[1][1]);
+                        for (int k = 0; k < 3; ++k) ldsm2t(b[k], sR + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
+                        mma16816(x0[n], tr[ki][0], b[0][0], b[0][1]);
+                        mma16816(x1[n], tr[ki][0], b[1][0], b[1][1]);
+                        mma16816(x2[n], tr[ki][1], b[1][0], b[1][1]);
+                        mma16816(x1[n], tr[ki][1], b[0][0], b[0][1]);
+                        mma16816(x2[n], tr[ki][0], b[2][0], b[2][1]);
+                        mma16816(x2[n], tr[ki][2], b[0][0], b[0][1]);
+                    }
+                }
+            uint32_t kc[4][4];   // key columns of the warp's share of the state, by 16 tokens
+#pragma unroll
+            for (int ki = 0; ki < 4; ++ki) {
+                const int row = ki * 16 + (lane & 15);
+                if (ND == 2) {
+                    const int unit = (warp & 3) * 2 + (lane >> 4);
+                    ldsm4t(kc[ki], smem_u32(s.k) + (warp >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
+                } else {
+                    uint32_t b2[2];
+                    ldsm2t(b2, smem_u32(s.k) + row * 128 + ((warp ^ (row & 7)) * 16));
+                    kc[ki][0] = b2[0]; kc[ki][1] = b2[1]; kc[ki][2] = kc[ki][3] = 0u;
                 }
             }
-            const float f0 = ex2(log2_between(s.csl[r0], end)), f1 = ex2(log2_between(s.csl[r1], end));
+            if (rows < Q)   // keys of other sequences, which may be anything, would meet zeros
+#pragma unroll
+                for (int ki = 0; ki < 4; ++ki)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int token = ki * 16 + t2 + 8 * (e & 1);
+                        kc[ki][e] &= (token < rows ? 0xffffu : 0u) | (token + 1 < rows ? 0xffff0000u : 0u);
+                    }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int cc = (n0 + n) * 8 + t2;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float a = x0[n][2 * h] + x1[n][2 * h], b = x0[n][2 * h + 1] + x1[n][2 * h + 1], f = h ? f1 : f0;
-                    uint32_t w[3], x[3];
+                    const float a = x0[n][2 * h] + (x1[n][2 * h] + x2[n][2 * h]), b = x0[n][2 * h + 1] + (x1[n][2 * h + 1] + x2[n][2 * h + 1]), f = h ? f1 : f0;
+                    uint32_t w[3];
                     split3(a * f, b * f, w[0], w[1], w[2]);
-                    split3(a, b, x[0], x[1], x[2]);
 #pragma unroll
                     for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.W[k][r0 + 8 * h][cc]) = w[k];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) *reinterpret_cast<uint32_t*>(&sm.X[k][r0 + 8 * h][cc]) = x[k];
+                    const uint32_t hi = pack_bf(a, b);
+                    *reinterpret_cast<uint32_t*>(&sm.X[0][r0 + 8 * h][cc]) = hi;
+                    *reinterpret_cast<uint32_t*>(&sm.X[1][r0 + 8 * h][cc]) = pack_bf(a - bf_lo(hi), b - bf_hi(hi));
                 }
             }
-        } else if (p.io.z && !ws.o) {
-            const __nv_bfloat16* z = static_cast<const __nv_bfloat16*>(p.io.z) + (size_t)(t0 + r0) * p.io.ldz + col;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                zr[n][0] = zr[n][1] = 0u;
-                if (r0 < rows) zr[n][0] = *reinterpret_cast<const uint32_t*>(z + (n0 + n) * 8 + t2);
-                if (r1 < rows) zr[n][1] = *reinterpret_cast<const uint32_t*>(z + 8 * p.io.ldz + (n0 + n) * 8 + t2);
-            }
-        }
-        __syncthreads();   // W and X are there; the state's operands have been read
-        if (!outputs) {
-            const float ec = ex2(end.x);
+            __syncthreads();   // W and X are there; the state's operands have been read
             float m[MS][ND][4];
 #pragma unroll
             for (int ms = 0; ms < MS; ++ms)
@@ -471,17 +557,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { S[ms][nd][e] *= ec; m[ms][nd][e] = 0.f; }
 #pragma unroll
-            for (int ki = 0; ki < Q / 16; ++ki) {
-                uint32_t b[4];
-                const int row = ki * 16 + (lane & 15);
-                if (ND == 2) {
-                    const int unit = (w8 & 3) * 2 + (lane >> 4);
-                    ldsm4t(b, sA + (w8 >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
-                } else {
-                    uint32_t b2[2];
-                    ldsm2t(b2, sA + row * 128 + ((w8 ^ (row & 7)) * 16));
-                    b[0] = b2[0]; b[1] = b2[1]; b[2] = b[3] = 0u;
-                }
+            for (int ki = 0; ki < Q / 16; ++ki)
 #pragma unroll
                 for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
@@ -489,8 +565,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                         uint32_t a[4];
                         ldsm4t(a, sW + ((k * Q + ki * 16 + (lane & 7) + ((lane >> 4) & 1) * 8) * kRow + ms * 16 + ((lane >> 3) & 1) * 8) * 2);
 #pragma unroll
-                        for (int nd = 0; nd < ND; ++nd) mma16816(k == 0 ? S[ms][nd] : m[ms][nd], a, b[2 * nd], b[2 * nd + 1]);
+                        for (int nd = 0; nd < ND; ++nd) mma16816(k == 0 ? S[ms][nd] : m[ms][nd], a, kc[ki][2 * nd], kc[ki][2 * nd + 1]);
                     }
+            if (c + 1 < nck) {
+                arrive(c + 1);
+                preload(c + 1);
             }
 #pragma unroll
             for (int ms = 0; ms < MS; ++ms)
@@ -499,35 +578,92 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
 #pragma unroll
                     for (int e = 0; e < 4; ++e) S[ms][nd][e] += m[ms][nd][e];
             store_split_state();
-        } else {
+            failed = __syncthreads_or(!here);   // the state's operands are there, the stage is free
+            if (failed) break;                  // a copy did not arrive in time
+        }
+        if (!failed && fslot >= 0 && (nck > 0 || fslot != islot)) {
+            float* h1 = p.pool.ssm + (size_t)fslot * p.pool.ssm_slot_stride + (size_t)col * DK;
+#pragma unroll
+            for (int ms = 0; ms < MS; ++ms)
+#pragma unroll
+                for (int nd = 0; nd < ND; ++nd) {
+                    const int c = (warp * ND + nd) * 8 + t2;
+                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g) * DK + c) = make_float2(S[ms][nd][0], S[ms][nd][1]);
+                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g + 8) * DK + c) = make_float2(S[ms][nd][2], S[ms][nd][3]);
+                }
+        }
+    } else {
+        uint32_t qr[KS][4];
+        auto preload = [&](int n) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) rows_operand(qr[ks], sm.stage[n % STAGES].q, ks);
+        };
+        if (nck > 0) {
+            arrive(0);
+            preload(0);
+        }
+        __syncthreads();
+        for (; c < nck; ++c) {
+            const ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+            const int t0 = s0 + c * Q, rows = len - c * Q;
             // O = scale e^G (Q S^T) + M X
-            float o[NT][4];
+            float o[NQ][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                o[n][0] = acc[0][n][0] * (e0 * p.L.scale); o[n][1] = acc[0][n][1] * (e0 * p.L.scale);
-                o[n][2] = acc[0][n][2] * (e1 * p.L.scale); o[n][3] = acc[0][n][3] * (e1 * p.L.scale);
-            }
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+#pragma unroll
+            for (int k2 = 0; k2 < KS / 2; ++k2)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    uint32_t b[4];
+                    state_operand(b, 0, n, k2);
+                    mma16816(o[n], qr[2 * k2], b[0], b[1]);
+                    mma16816(o[n], qr[2 * k2 + 1], b[2], b[3]);
+                }
+            uint32_t mr[4][4], zr[NQ][2];
             const uint32_t sM = smem_u32(s.M) + (mt * (mt + 1) / 2) * 512 + lane * 16;
-            for (int ki = 0; ki <= mt; ++ki) {
-                uint32_t a[4];
-                lds16(a, sM + ki * 512);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int ki = 0; ki < 4; ++ki)
+                if (ki <= mt) lds16(mr[ki], sM + ki * 512);
+            if (p.io.z && !ws.o) {
+                const __nv_bfloat16* z = static_cast<const __nv_bfloat16*>(p.io.z) + (size_t)(t0 + r0) * p.io.ldz + col;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        uint32_t b[2];
-                        ldsm2t(b, sX + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
-                        mma16816(o[n], a, b[0], b[1]);
-                    }
+                for (int n = 0; n < NQ; ++n) {
+                    zr[n][0] = zr[n][1] = 0u;
+                    if (r0 < rows) zr[n][0] = *reinterpret_cast<const uint32_t*>(z + n * 8 + t2);
+                    if (r1 < rows) zr[n][1] = *reinterpret_cast<const uint32_t*>(z + 8 * p.io.ldz + n * 8 + t2);
+                }
+            }
+            const float e0 = ex2(s.csl[r0].x) * p.L.scale, e1 = ex2(s.csl[r1].x) * p.L.scale;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) { o[n][0] *= e0; o[n][1] *= e0; o[n][2] *= e1; o[n][3] *= e1; }
+            __syncthreads();   // X is there; the state's operands have been read
+#pragma unroll
+            for (int ki = 0; ki < 4; ++ki)
+                if (ki <= mt) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int n2 = 0; n2 < NQ / 2; ++n2) {
+                            uint32_t b[4];
+                            ldsm4t(b, sX + ((k * Q + ki * 16 + (lane & 15)) * kRow + n2 * 16 + (lane >> 4) * 8) * 2);
+                            mma16816(o[2 * n2], mr[ki], b[0], b[1]);
+                            mma16816(o[2 * n2 + 1], mr[ki], b[2], b[3]);
+                        }
+                }
+            if (c + 1 < nck) {
+                arrive(c + 1);
+                preload(c + 1);
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = r0 + 8 * h;
                     if (r >= rows) continue;
                     const size_t t = (size_t)(t0 + r);
-                    const int cc = col + (n0 + n) * 8 + t2;
+                    const int cc = col + n * 8 + t2;
                     float a = o[n][2 * h], b = o[n][2 * h + 1];
                     if (ws.o) {
                         *reinterpret_cast<float2*>(ws.o + t * (H * d_v) + cc) = make_float2(a, b);
@@ -536,30 +672,17 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                         *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.io.out) + t * p.io.ldo + cc) = pack_bf(a, b);
                     }
                 }
+            failed = __syncthreads_or(!here);
+            if (failed) break;
+            if (tid == kChainThreads - 32 && c + STAGES < nck) fetch(c + STAGES, c % STAGES);
         }
-        // the state's operands are there, the stage is free
-        if (__syncthreads_or(!here)) {   // a copy did not arrive in time
-            if (tid == 0) {
-                flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
-                for (int i = c; i < c + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
-            }
-            __syncthreads();
-            return;
-        }
-        if (tid == kChainThreads - 32 && c + STAGES < nck) fetch(c + STAGES, st);
     }
-    if (!outputs && fslot >= 0 && (nck > 0 || fslot != islot)) {
-        float* h1 = p.pool.ssm + (size_t)fslot * p.pool.ssm_slot_stride + (size_t)col * DK;
-#pragma unroll
-        for (int ms = 0; ms < MS; ++ms)
-#pragma unroll
-            for (int nd = 0; nd < ND; ++nd) {
-                const int c = (w8 * ND + nd) * 8 + t2;
-                *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g) * DK + c) = make_float2(S[ms][nd][0], S[ms][nd][1]);
-                *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g + 8) * DK + c) = make_float2(S[ms][nd][2], S[ms][nd][3]);
-            }
+    if (failed && tid == 0) {   // copies target this block's shared memory: one more bounded chance
+        flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
+        for (int i = c; i < c + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
     }
 }
+
 
 // ---------------------------------------------------------------- kernel 3: output norm and gate, a warp per row and head
 constexpr int kNormThreads = 256;
