@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
 }
 
 // ---------------------------------------------------------------- kernel 2
-constexpr int kChainThreads = 384;   // warps 0-7: the state's products; warps 8-11: the outputs'
+constexpr int kChainThreads = 256;   // warps 0-3: the state's products; warps 4-7: the outputs'
 
 template <int DK, int DVS>
 struct ChainStage {
@@ -288,10 +288,11 @@ template <int DK, int DVS, int STAGES>
 struct ChainSmem {
     static constexpr int kRow = DVS + 8;                // values of a row of the operands below, padded against bank conflicts
     ChainStage<DK, DVS> stage[STAGES];
-    __nv_bfloat16 S[3][DVS][DK];                        // state split in three, 16-byte units XOR-ed with the row index
-    __nv_bfloat16 R[3][Q][kRow];                        // beta^-1 of what is written, split in three
+    float4 part[4][3][DVS / 8][32];                     // K S^T over a warp's share of d_k, for the warps of the other row tiles
+    __nv_bfloat16 S[2][DVS][DK];                        // leading part of the incoming state, by parity of the chunk; 16-byte units XOR-ed with the row index
+    __nv_bfloat16 R[3][Q][kRow];                        // V - e^G (K S^T), split in three
     __nv_bfloat16 W[3][Q][kRow];                        // e^{G_end - G} X, split in three
-    __nv_bfloat16 X[2][Q][kRow];                        // X, split in two
+    __nv_bfloat16 X[2][2][Q][kRow];                     // X, split in two, by parity
     uint64_t full[STAGES];
 };
 
@@ -313,21 +314,22 @@ __device__ __forceinline__ void lds16(uint32_t (&r)[4], uint32_t a) {
 }
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// The state's warps load what does not depend on the product ahead of it before the barrier in between: the next chunk's key rows, the rows of T,
-// the key columns of the update.  (With every operand loaded behind its barrier a chunk of 128 x 128 took 4100 cycles instead of ???.)
+// A state warp holds DVS x DK / 4 of the state as accumulators of the update; split in three they are, as they lie, the operands of its share of K S^T
+// (a quarter of d_k, all 64 tokens), so the state never passes through shared memory; the four partial sums do, to the warp of each row tile.
+// What does not depend on the product ahead is loaded before the barrier in between.  The output warps trail by half a chunk.
 template <int DK, int DVS, int STAGES>
 __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps, int d_v) {
     using Smem = ChainSmem<DK, DVS, STAGES>;
     constexpr int kRow = Smem::kRow;
-    constexpr int NT = DVS / 16;        // 8-column tiles of a state warp in products of 64 x DVS
-    constexpr int NQ = DVS / 8;         // and of an output warp
+    constexpr int NT = DVS / 8;         // 8-column tiles of a product of 64 x DVS
+    constexpr int NX = NT / 2;          // of which a state warp has these of each of two row tiles in T R
     constexpr int MS = DVS / 16;        // 16-row tiles of the state slice
-    constexpr int ND = DK / 64;         // 8-column tiles of a warp in the state slice
+    constexpr int ND = DK / 32;         // 8-column tiles of a warp in the state slice
     constexpr int KS = DK / 16;         // steps over d_k
     extern __shared__ __align__(1024) unsigned char s_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool outputs = warp >= 8;
+    const bool outputs = warp >= 4;
     const int slice = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
     grid_release_dependents();
     int first, nck, s0, len;
@@ -350,38 +352,33 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
     }
     grid_wait();   // T, M and the running decays are the work of the kernel just before
     __syncthreads();
-    auto fetch = [&](int c, int st) {   // one thread
-        ChainStage<DK, DVS>& s = sm.stage[st];
-        const int t0 = s0 + c * Q;
-        const size_t ch = (size_t)(first + c) * H + head;
-        mbar_expect_tx(&sm.full[st], 2 * Q * DK * 2 + kTBytes + kMBytes + Q * DVS * 2 + Q * 8);
+    auto fetch = [&](int n) {   // one thread
+        ChainStage<DK, DVS>& s = sm.stage[n % STAGES];
+        uint64_t* bar = &sm.full[n % STAGES];
+        const size_t ch = (size_t)(first + n) * H + head;
+        mbar_expect_tx(bar, 2 * Q * DK * 2 + kTBytes + kMBytes + Q * DVS * 2 + Q * 8);
 #pragma unroll
         for (int h = 0; h < DK / 64; ++h) {
-            tma_box(s.k + h * 8192, &maps.k, khead * DK + 64 * h, t0, &sm.full[st]);
-            tma_box(s.q + h * 8192, &maps.q, khead * DK + 64 * h, t0, &sm.full[st]);
+            tma_box(s.k + h * 8192, &maps.k, khead * DK + 64 * h, s0 + n * Q, bar);
+            tma_box(s.q + h * 8192, &maps.q, khead * DK + 64 * h, s0 + n * Q, bar);
         }
-        tma_box(s.v, &maps.v, col, t0, &sm.full[st]);
-        bulk_load(s.T, ws.T + ch * kTBytes, kTBytes, &sm.full[st]);
-        bulk_load(s.M, ws.M + ch * kMBytes, kMBytes, &sm.full[st]);
-        bulk_load(s.csl, ws.csl + ch * Q, Q * 8, &sm.full[st]);
+        tma_box(s.v, &maps.v, col, s0 + n * Q, bar);
+        bulk_load(s.T, ws.T + ch * kTBytes, kTBytes, bar);
+        bulk_load(s.M, ws.M + ch * kMBytes, kMBytes, bar);
+        bulk_load(s.csl, ws.csl + ch * Q, Q * 8, bar);
     };
     if (tid == kChainThreads - 32)
-        for (int i = 0; i < STAGES && i < nck; ++i) fetch(i, i);
+#pragma unroll 1
+        for (int i = 0; i < STAGES && i < nck; ++i) fetch(i);
 
     const int g = lane >> 2, t2 = 2 * (lane & 3);
-    const uint32_t sS = smem_u32(sm.S), sR = smem_u32(sm.R), sW = smem_u32(sm.W), sX = smem_u32(sm.X);
-    // Row tile and column tiles of the warp in products of 64 x DVS; the triangles' work is even over the schedulers (warps w and w + 4).
-    const int mt = outputs ? warp - 8 : (warp < 4 ? warp : 7 - warp), n0 = outputs ? 0 : (warp >> 2) * NT;
+    const uint32_t sR = smem_u32(sm.R), sW = smem_u32(sm.W);
+    const int mt = warp & 3;   // row tile of the warp in products of 64 x DVS
     const int r0 = mt * 16 + g, r1 = r0 + 8;
     // Operand of 16 rows of keys or queries, step ks of d_k.
-    auto rows_operand = [&](uint32_t (&a)[4], const unsigned char* m, int ks) {
-        const int row = mt * 16 + (lane & 15), unit = (ks & 3) * 2 + (lane >> 4);
+    auto rows_operand = [&](uint32_t (&a)[4], const unsigned char* m, int tile, int ks) {
+        const int row = tile * 16 + (lane & 15), unit = (ks & 3) * 2 + (lane >> 4);
         ldsm4(a, smem_u32(m) + (ks >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
-    };
-    // Operand of 8 values of the state, steps 2 k2 and 2 k2 + 1 of d_k.
-    auto state_operand = [&](uint32_t (&b)[4], int part, int n, int k2) {
-        const int row = n * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
-        ldsm4(b, sS + (part * DVS + row) * (DK * 2) + ((unit ^ (row & 7)) * 16));
     };
     bool here = true, failed = false;
     int c = 0;
@@ -397,158 +394,182 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
 #pragma unroll
                 for (int nd = 0; nd < ND; ++nd) {
                     float2 a = make_float2(0.f, 0.f), b = a;
-                    const int c = (warp * ND + nd) * 8 + t2;
+                    const int d = (warp * ND + nd) * 8 + t2;
                     if (islot >= 0) {
-                        a = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g) * DK + c);
-                        b = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g + 8) * DK + c);
+                        a = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g) * DK + d);
+                        b = *reinterpret_cast<const float2*>(h0 + (size_t)(ms * 16 + g + 8) * DK + d);
                     }
                     S[ms][nd][0] = a.x; S[ms][nd][1] = a.y; S[ms][nd][2] = b.x; S[ms][nd][3] = b.y;
                 }
         }
-        auto store_split_state = [&] {
+        // The state as operands: part, tile of 8 rows, tile of 8 columns; its leading part goes to the output warps too.
+        uint32_t sp[3][NT][ND];
+        auto split_state = [&](int parity) {
 #pragma unroll
             for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
                 for (int nd = 0; nd < ND; ++nd)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const int row = ms * 16 + g + 8 * h, unit = warp * ND + nd;
-                        uint32_t s[3];
-                        split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], s[0], s[1], s[2]);
-#pragma unroll
-                        for (int k = 0; k < 3; ++k)
-                            *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[k][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = s[k];
+                        const int n = 2 * ms + h, row = n * 8 + g, unit = warp * ND + nd;
+                        split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], sp[0][n][nd], sp[1][n][nd], sp[2][n][nd]);
+                        *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[parity][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = sp[0][n][nd];
                     }
         };
-        store_split_state();
-        uint32_t kr[KS][4];        // key rows of the chunk
-        uint32_t vr[NT][2];        // values
-        float e0 = 0.f, e1 = 0.f, f0 = 0.f, f1 = 0.f, ec = 0.f;
-        auto preload = [&](int c) {
-            const ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+        split_state(0);
+        constexpr int KW = KS / 4;   // the warp's steps over d_k
+        uint32_t kr[4][KW][4];       // its keys: all rows of the chunk
+        uint32_t vr[NT][2];          // values of row tile mt
+        float e0 = 0.f, e1 = 0.f, ec = 0.f;
+        // T R takes half the columns of row tile mt and the other half of row tile 3 - mt, five blocks of the triangle for every warp: first the
+        // shorter row of blocks (one or two), then the longer.
+        const int m_of[2] = {mt < 2 ? mt : 3 - mt, mt < 2 ? 3 - mt : mt}, n_of[2] = {mt < 2 ? 0 : NX, mt < 2 ? NX : 0};
+        float fr[2][2] = {{0.f, 0.f}, {0.f, 0.f}};   // decay from their rows to the chunk's end
+        auto preload = [&](int n) {
+            const ChainStage<DK, DVS>& s = sm.stage[n % STAGES];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) rows_operand(kr[ks], s.k, ks);
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                vr[n][0] = *reinterpret_cast<const uint32_t*>(&s.v[r0][(n0 + n) * 8 + t2]);
-                vr[n][1] = *reinterpret_cast<const uint32_t*>(&s.v[r1][(n0 + n) * 8 + t2]);
+                for (int j = 0; j < KW; ++j) rows_operand(kr[m][j], s.k, m, warp * KW + j);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                vr[i][0] = *reinterpret_cast<const uint32_t*>(&s.v[r0][i * 8 + t2]);
+                vr[i][1] = *reinterpret_cast<const uint32_t*>(&s.v[r1][i * 8 + t2]);
             }
             const float2 end = s.csl[Q - 1], c0 = s.csl[r0], c1 = s.csl[r1];
             e0 = ex2(c0.x); e1 = ex2(c1.x); ec = ex2(end.x);
-            f0 = ex2(log2_between(c0, end)); f1 = ex2(log2_between(c1, end));
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fr[i][h] = ex2(log2_between(s.csl[m_of[i] * 16 + g + 8 * h], end));
         };
         if (nck > 0) {
             arrive(0);
             preload(0);
         }
-        __syncthreads();
         for (; c < nck; ++c) {
             ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
             const int rows = len - c * Q;
-            // K S^T, a product per part of the state
-            float acc[3][NT][4];
+            // K S^T over the warp's share of d_k
+            float d[4][NT][4];
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[k][n][e] = 0.f;
+                    for (int e = 0; e < 4; ++e) d[m][n][e] = 0.f;
 #pragma unroll
-            for (int k2 = 0; k2 < KS / 2; ++k2)
+            for (int k = 2; k >= 0; --k)
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
+                for (int j = 0; j < KW; ++j)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t b[4];
-                        state_operand(b, k, n0 + n, k2);
-                        mma16816(acc[k][n], kr[2 * k2], b[0], b[1]);
-                        mma16816(acc[k][n], kr[2 * k2 + 1], b[2], b[3]);
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816(d[m][n], kr[m][j], sp[k][n][2 * j], sp[k][n][2 * j + 1]);
+            float own[NT][4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (m == warp) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) own[n][e] = d[m][n][e];
+                    } else {
+                        sm.part[m][(warp - m - 1) & 3][n][lane] = make_float4(d[m][n][0], d[m][n][1], d[m][n][2], d[m][n][3]);
                     }
-            uint32_t tr[4][3][4];   // rows of T, blocks up to the diagonal (what lies behind is not used)
-            const uint32_t sT = smem_u32(s.T) + (mt * (mt + 1) / 2) * 512 + lane * 16;
-#pragma unroll
-            for (int ki = 0; ki < 4; ++ki)
-                if (ki <= mt)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) lds16(tr[ki][k], sT + (k * kBlocks + ki) * 512);
+                }
+            bar_sync(1, 128);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int cc = (n0 + n) * 8 + t2;
-                float d[4];
+                const int cc = n * 8 + t2;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] = (acc[2][n][e] + acc[1][n][e]) + acc[0][n][e];
-                d[0] = r0 < rows ? fmaf(-e0, d[0], bf_lo(vr[n][0])) : 0.f;
-                d[1] = r0 < rows ? fmaf(-e0, d[1], bf_hi(vr[n][0])) : 0.f;
-                d[2] = r1 < rows ? fmaf(-e1, d[2], bf_lo(vr[n][1])) : 0.f;
-                d[3] = r1 < rows ? fmaf(-e1, d[3], bf_hi(vr[n][1])) : 0.f;
+                for (int i = 0; i < 3; ++i) {
+                    const float4 o = sm.part[mt][i][n][lane];
+                    own[n][0] += o.x; own[n][1] += o.y; own[n][2] += o.z; own[n][3] += o.w;
+                }
+                own[n][0] = r0 < rows ? fmaf(-e0, own[n][0], bf_lo(vr[n][0])) : 0.f;
+                own[n][1] = r0 < rows ? fmaf(-e0, own[n][1], bf_hi(vr[n][0])) : 0.f;
+                own[n][2] = r1 < rows ? fmaf(-e1, own[n][2], bf_lo(vr[n][1])) : 0.f;
+                own[n][3] = r1 < rows ? fmaf(-e1, own[n][3], bf_hi(vr[n][1])) : 0.f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[3];
-                    split3(d[2 * h], d[2 * h + 1], x[0], x[1], x[2]);
+                    split3(own[n][2 * h], own[n][2 * h + 1], x[0], x[1], x[2]);
 #pragma unroll
                     for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.R[k][r0 + 8 * h][cc]) = x[k];
                 }
             }
-            bar_sync(1, 256);
+            bar_sync(1, 128);
             // X = T R, the six products that reach 24 bits
-            float x0[NT][4], x1[NT][4], x2[NT][4];
+            float x[NX][3][4], xs[NX][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NX; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x0[n][e] = x1[n][e] = x2[n][e] = 0.f;
+                for (int e = 0; e < 4; ++e) { x[n][0][e] = x[n][1][e] = x[n][2][e] = 0.f; xs[n][e] = 0.f; }
 #pragma unroll
-            for (int ki = 0; ki < 4; ++ki)
-                if (ki <= mt) {
+            for (int j = 0; j < 5; ++j) {
+                const bool i = j > m_of[0];
+                const int ki = i ? j - m_of[0] - 1 : j, mi = i ? m_of[1] : m_of[0], ni = i ? n_of[1] : n_of[0];
+                uint32_t t[3][4], b[NX][3][2];
+                const uint32_t sT = smem_u32(s.T) + (mi * (mi + 1) / 2 + ki) * 512 + lane * 16, sB = sR + ((ki * 16 + (lane & 15)) * kRow + ni * 8) * 2;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t b[3][2];
+                for (int k = 0; k < 3; ++k) {
+                    lds16(t[k], sT + k * kBlocks * 512);
 #pragma unroll
-                        for (int k = 0; k < 3; ++k) ldsm2t(b[k], sR + ((k * Q + ki * 16 + (lane & 15)) * kRow + (n0 + n) * 8) * 2);
-                        mma16816(x0[n], tr[ki][0], b[0][0], b[0][1]);
-                        mma16816(x1[n], tr[ki][0], b[1][0], b[1][1]);
-                        mma16816(x2[n], tr[ki][1], b[1][0], b[1][1]);
-                        mma16816(x1[n], tr[ki][1], b[0][0], b[0][1]);
-                        mma16816(x2[n], tr[ki][0], b[2][0], b[2][1]);
-                        mma16816(x2[n], tr[ki][2], b[0][0], b[0][1]);
-                    }
+                    for (int n = 0; n < NX; ++n) ldsm2t(b[n][k], sB + (k * Q * kRow + n * 8) * 2);
                 }
-            uint32_t kc[4][4];   // key columns of the warp's share of the state, by 16 tokens
 #pragma unroll
-            for (int ki = 0; ki < 4; ++ki) {
-                const int row = ki * 16 + (lane & 15);
-                if (ND == 2) {
-                    const int unit = (warp & 3) * 2 + (lane >> 4);
-                    ldsm4t(kc[ki], smem_u32(s.k) + (warp >> 2) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
-                } else {
-                    uint32_t b2[2];
-                    ldsm2t(b2, smem_u32(s.k) + row * 128 + ((warp ^ (row & 7)) * 16));
-                    kc[ki][0] = b2[0]; kc[ki][1] = b2[1]; kc[ki][2] = kc[ki][3] = 0u;
+                for (int n = 0; n < NX; ++n) {
+                    mma16816(x[n][0], t[0], b[n][0][0], b[n][0][1]);
+                    mma16816(x[n][1], t[0], b[n][1][0], b[n][1][1]);
+                    mma16816(x[n][2], t[1], b[n][1][0], b[n][1][1]);
+                    mma16816(x[n][1], t[1], b[n][0][0], b[n][0][1]);
+                    mma16816(x[n][2], t[0], b[n][2][0], b[n][2][1]);
+                    mma16816(x[n][0], t[2], b[n][0][0], b[n][0][1]);
                 }
+                if (j < 2 && j == m_of[0])   // the shorter row of blocks is complete
+#pragma unroll
+                    for (int n = 0; n < NX; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            xs[n][e] = (x[n][2][e] + x[n][1][e]) + x[n][0][e];
+                            x[n][0][e] = x[n][1][e] = x[n][2][e] = 0.f;
+                        }
             }
-            if (rows < Q)   // keys of other sequences, which may be anything, would meet zeros
 #pragma unroll
-                for (int ki = 0; ki < 4; ++ki)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int token = ki * 16 + t2 + 8 * (e & 1);
-                        kc[ki][e] &= (token < rows ? 0xffffu : 0u) | (token + 1 < rows ? 0xffff0000u : 0u);
+                for (int n = 0; n < NX; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int cc = (n_of[i] + n) * 8 + t2, row = m_of[i] * 16 + g + 8 * h;
+                        const float v0 = i ? (x[n][2][2 * h] + x[n][1][2 * h]) + x[n][0][2 * h] : xs[n][2 * h];
+                        const float v1 = i ? (x[n][2][2 * h + 1] + x[n][1][2 * h + 1]) + x[n][0][2 * h + 1] : xs[n][2 * h + 1];
+                        uint32_t w[3];
+                        split3(v0 * fr[i][h], v1 * fr[i][h], w[0], w[1], w[2]);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.W[k][row][cc]) = w[k];
+                        const uint32_t hi = pack_bf(v0, v1);
+                        *reinterpret_cast<uint32_t*>(&sm.X[c & 1][0][row][cc]) = hi;
+                        *reinterpret_cast<uint32_t*>(&sm.X[c & 1][1][row][cc]) = pack_bf(v0 - bf_lo(hi), v1 - bf_hi(hi));
                     }
+            uint32_t kc[ND / 2][4];   // key columns of the warp's share of the state, 16 tokens at a time
+            auto load_keys = [&](int ki) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int cc = (n0 + n) * 8 + t2;
+                for (int j = 0; j < ND / 2; ++j) {
+                    const int row = ki * 16 + (lane & 15), u = warp * ND + 2 * j, unit = (u & 7) + (lane >> 4);
+                    ldsm4t(kc[j], smem_u32(s.k) + (u >> 3) * 8192 + row * 128 + ((unit ^ (row & 7)) * 16));
+                    if (rows < Q)   // keys of other sequences, which may be anything, would meet zeros
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float a = x0[n][2 * h] + (x1[n][2 * h] + x2[n][2 * h]), b = x0[n][2 * h + 1] + (x1[n][2 * h + 1] + x2[n][2 * h + 1]), f = h ? f1 : f0;
-                    uint32_t w[3];
-                    split3(a * f, b * f, w[0], w[1], w[2]);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.W[k][r0 + 8 * h][cc]) = w[k];
-                    const uint32_t hi = pack_bf(a, b);
-                    *reinterpret_cast<uint32_t*>(&sm.X[0][r0 + 8 * h][cc]) = hi;
-                    *reinterpret_cast<uint32_t*>(&sm.X[1][r0 + 8 * h][cc]) = pack_bf(a - bf_lo(hi), b - bf_hi(hi));
+                        for (int e = 0; e < 4; ++e) {
+                            const int token = ki * 16 + t2 + 8 * (e & 1);
+                            kc[j][e] &= (token < rows ? 0xffffu : 0u) | (token + 1 < rows ? 0xffff0000u : 0u);
+                        }
                 }
-            }
-            __syncthreads();   // W and X are there; the state's operands have been read
+            };
+            load_keys(0);
+            failed = __syncthreads_or(!here);   // W, X and the state's leading part are there; the output warps are done with the chunk before
+            if (failed) break;                  // a copy did not arrive in time
             float m[MS][ND][4];
 #pragma unroll
             for (int ms = 0; ms < MS; ++ms)
@@ -556,8 +577,8 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 for (int nd = 0; nd < ND; ++nd)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { S[ms][nd][e] *= ec; m[ms][nd][e] = 0.f; }
-#pragma unroll
-            for (int ki = 0; ki < Q / 16; ++ki)
+#pragma unroll 1
+            for (int ki = 0; ki < Q / 16; ++ki) {
 #pragma unroll
                 for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
@@ -565,8 +586,10 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                         uint32_t a[4];
                         ldsm4t(a, sW + ((k * Q + ki * 16 + (lane & 7) + ((lane >> 4) & 1) * 8) * kRow + ms * 16 + ((lane >> 3) & 1) * 8) * 2);
 #pragma unroll
-                        for (int nd = 0; nd < ND; ++nd) mma16816(k == 0 ? S[ms][nd] : m[ms][nd], a, kc[ki][2 * nd], kc[ki][2 * nd + 1]);
+                        for (int nd = 0; nd < ND; ++nd) mma16816(k == 0 ? S[ms][nd] : m[ms][nd], a, kc[nd / 2][2 * (nd & 1)], kc[nd / 2][2 * (nd & 1) + 1]);
                     }
+                if (ki + 1 < Q / 16) load_keys(ki + 1);
+            }
             if (c + 1 < nck) {
                 arrive(c + 1);
                 preload(c + 1);
@@ -577,9 +600,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 for (int nd = 0; nd < ND; ++nd)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) S[ms][nd][e] += m[ms][nd][e];
-            store_split_state();
-            failed = __syncthreads_or(!here);   // the state's operands are there, the stage is free
-            if (failed) break;                  // a copy did not arrive in time
+            if (c + 1 < nck) split_state((c + 1) & 1);
         }
         if (!failed && fslot >= 0 && (nck > 0 || fslot != islot)) {
             float* h1 = p.pool.ssm + (size_t)fslot * p.pool.ssm_slot_stride + (size_t)col * DK;
@@ -587,41 +608,19 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
             for (int ms = 0; ms < MS; ++ms)
 #pragma unroll
                 for (int nd = 0; nd < ND; ++nd) {
-                    const int c = (warp * ND + nd) * 8 + t2;
-                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g) * DK + c) = make_float2(S[ms][nd][0], S[ms][nd][1]);
-                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g + 8) * DK + c) = make_float2(S[ms][nd][2], S[ms][nd][3]);
+                    const int d = (warp * ND + nd) * 8 + t2;
+                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g) * DK + d) = make_float2(S[ms][nd][0], S[ms][nd][1]);
+                    *reinterpret_cast<float2*>(h1 + (size_t)(ms * 16 + g + 8) * DK + d) = make_float2(S[ms][nd][2], S[ms][nd][3]);
                 }
         }
     } else {
-        uint32_t qr[KS][4];
-        auto preload = [&](int n) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) rows_operand(qr[ks], sm.stage[n % STAGES].q, ks);
-        };
-        if (nck > 0) {
-            arrive(0);
-            preload(0);
-        }
-        __syncthreads();
         for (; c < nck; ++c) {
             const ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
             const int t0 = s0 + c * Q, rows = len - c * Q;
-            // O = scale e^G (Q S^T) + M X
-            float o[NQ][4];
+            arrive(c);
+            uint32_t qr[KS][4], mr[4][4], zr[NT][2];
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-#pragma unroll
-            for (int k2 = 0; k2 < KS / 2; ++k2)
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    uint32_t b[4];
-                    state_operand(b, 0, n, k2);
-                    mma16816(o[n], qr[2 * k2], b[0], b[1]);
-                    mma16816(o[n], qr[2 * k2 + 1], b[2], b[3]);
-                }
-            uint32_t mr[4][4], zr[NQ][2];
+            for (int ks = 0; ks < KS; ++ks) rows_operand(qr[ks], s.q, mt, ks);
             const uint32_t sM = smem_u32(s.M) + (mt * (mt + 1) / 2) * 512 + lane * 16;
 #pragma unroll
             for (int ki = 0; ki < 4; ++ki)
@@ -629,35 +628,50 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
             if (p.io.z && !ws.o) {
                 const __nv_bfloat16* z = static_cast<const __nv_bfloat16*>(p.io.z) + (size_t)(t0 + r0) * p.io.ldz + col;
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) {
+                for (int n = 0; n < NT; ++n) {
                     zr[n][0] = zr[n][1] = 0u;
                     if (r0 < rows) zr[n][0] = *reinterpret_cast<const uint32_t*>(z + n * 8 + t2);
                     if (r1 < rows) zr[n][1] = *reinterpret_cast<const uint32_t*>(z + 8 * p.io.ldz + n * 8 + t2);
                 }
             }
             const float e0 = ex2(s.csl[r0].x) * p.L.scale, e1 = ex2(s.csl[r1].x) * p.L.scale;
+            failed = __syncthreads_or(!here);   // X and the state's leading part are there
+            if (failed) break;
+            if (tid == kChainThreads - 32 && c > 0 && c - 1 + STAGES < nck) fetch(c - 1 + STAGES);   // all warps are done with the chunk before
+            // O = scale e^G (Q S^T) + M X
+            float o[NT][4];
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) { o[n][0] *= e0; o[n][1] *= e0; o[n][2] *= e1; o[n][3] *= e1; }
-            __syncthreads();   // X is there; the state's operands have been read
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+            const uint32_t sS = smem_u32(sm.S[c & 1]), sX = smem_u32(sm.X[c & 1]);
+#pragma unroll
+            for (int k2 = 0; k2 < KS / 2; ++k2)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t b[4];
+                    const int row = n * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
+                    ldsm4(b, sS + row * (DK * 2) + ((unit ^ (row & 7)) * 16));
+                    mma16816(o[n], qr[2 * k2], b[0], b[1]);
+                    mma16816(o[n], qr[2 * k2 + 1], b[2], b[3]);
+                }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) { o[n][0] *= e0; o[n][1] *= e0; o[n][2] *= e1; o[n][3] *= e1; }
 #pragma unroll
             for (int ki = 0; ki < 4; ++ki)
                 if (ki <= mt) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
-                        for (int n2 = 0; n2 < NQ / 2; ++n2) {
+                        for (int n2 = 0; n2 < NT / 2; ++n2) {
                             uint32_t b[4];
                             ldsm4t(b, sX + ((k * Q + ki * 16 + (lane & 15)) * kRow + n2 * 16 + (lane >> 4) * 8) * 2);
                             mma16816(o[2 * n2], mr[ki], b[0], b[1]);
                             mma16816(o[2 * n2 + 1], mr[ki], b[2], b[3]);
                         }
                 }
-            if (c + 1 < nck) {
-                arrive(c + 1);
-                preload(c + 1);
-            }
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = r0 + 8 * h;
@@ -672,17 +686,13 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                         *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.io.out) + t * p.io.ldo + cc) = pack_bf(a, b);
                     }
                 }
-            failed = __syncthreads_or(!here);
-            if (failed) break;
-            if (tid == kChainThreads - 32 && c + STAGES < nck) fetch(c + STAGES, c % STAGES);
         }
     }
     if (failed && tid == 0) {   // copies target this block's shared memory: one more bounded chance
         flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
-        for (int i = c; i < c + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
+        for (int i = c > 0 ? c - 1 : 0; i < (c > 0 ? c - 1 : 0) + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
     }
 }
-
 
 // ---------------------------------------------------------------- kernel 3: output norm and gate, a warp per row and head
 constexpr int kNormThreads = 256;
