@@ -1044,11 +1044,12 @@ GdrPlan plan_gdr(const mdraft_gdr_layer* L, int T, int n_seq, int max_seqlen) {
     if (!pl.chunked) return pl;
     pl.n_chunks_bound = n_seq + T / kGdrQ;
     const size_t n = (size_t)pl.n_chunks_bound * L->n_v_heads;
-    pl.slice = (int64_t)n_seq * L->n_v_heads * (L->d_v / 16) <= sm_count() ? 16 : 32;
-    pl.off_M = align_up(n * kGdrTBytes, 256);
-    pl.off_csl = align_up(pl.off_M + n * kGdrMBytes, 256);
+    pl.slice = (int64_t)n_seq * L->n_v_heads * (L->d_v / 16) <= sm_count() ? 16 : L->d_v;
+    const bool wide = pl.slice == L->d_v;
+    pl.off_M = align_up(n * (wide ? kGdrWideTBytes : kGdrTBytes), 256);
+    pl.off_csl = align_up(pl.off_M + n * (wide ? kGdrWideMBytes : kGdrMBytes), 256);
     pl.off_o = align_up(pl.off_csl + n * kGdrQ * sizeof(float2), 256);
-    pl.bytes = align_up(pl.off_o + (L->norm_w ? (size_t)T * L->n_v_heads * L->d_v * sizeof(float) : 0), 256);
+    pl.bytes = align_up(pl.off_o + (L->norm_w && !wide ? (size_t)T * L->n_v_heads * L->d_v * sizeof(float) : 0), 256);
     return pl;
 }
 
@@ -1111,11 +1112,13 @@ int mdraft_gdr_prefill(const mdraft_gdr_layer* layer, const mdraft_cache* cache,
         if (reinterpret_cast<uintptr_t>(workspace) & 255u) return MDRAFT_ERR_MISALIGNED;
         a.n_chunks_bound = pl.n_chunks_bound;
         unsigned char* w = static_cast<unsigned char*>(workspace);
-        const GdrChunkWs ws = {w, w + pl.off_M, reinterpret_cast<float2*>(w + pl.off_csl), layer->norm_w ? reinterpret_cast<float*>(w + pl.off_o) : nullptr};
+        const GdrChunkWs ws = {w, w + pl.off_M, reinterpret_cast<float2*>(w + pl.off_csl), layer->norm_w && pl.slice < layer->d_v ? reinterpret_cast<float*>(w + pl.off_o) : nullptr};
         GdrMaps maps;
+        memset(&maps.z, 0, sizeof(maps.z));
         const int64_t kc = (int64_t)layer->n_k_heads * layer->d_k, vc = (int64_t)layer->n_v_heads * layer->d_v;
         if (!encode_gdr_matrix(&maps.q, q, total_tokens, kc, ldq, 64, true) || !encode_gdr_matrix(&maps.k, k, total_tokens, kc, ldk, 64, true) ||
-            !encode_gdr_matrix(&maps.v, v, total_tokens, vc, ldv, pl.slice, false))
+            !encode_gdr_matrix(&maps.v, v, total_tokens, vc, ldv, pl.slice, false) ||
+            (z && pl.slice == layer->d_v && !encode_gdr_matrix(&maps.z, z, total_tokens, vc, ldz, pl.slice, false)))
             return MDRAFT_ERR_CUDA;
         return launch_gdr_chunked(a, ws, maps, layer->d_k, layer->d_v, pl.slice, st) == cudaSuccess ? MDRAFT_OK : MDRAFT_ERR_CUDA;
     }

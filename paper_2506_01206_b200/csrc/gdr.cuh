@@ -40,20 +40,23 @@ cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int
 
 // Scratch of the chunked encode, per (chunk, value head).
 constexpr uint32_t kGdrTBytes = 15360, kGdrMBytes = 5120;   // lower triangles in 16 x 16 blocks, as the chain's lanes hold them
+constexpr uint32_t kGdrWideTBytes = 24576, kGdrWideMBytes = 8192;   // the wide chain's: 64 rows of 128 bytes, 128-byte swizzle (three of them for T)
 struct GdrChunkWs {
     unsigned char* T;   // (1 + A)^-1 diag(beta), split into three bf16 values
-    unsigned char* M;   // masked products of queries and keys, bf16
-    float2* csl;        // 64 running log2 decays (value, remainder)
-    float* o;           // (T, Hv * d_v) fp32 outputs before the norm; NULL: there is no norm
+    unsigned char* M;   // masked products of queries and keys, bf16; for the wide chain times T
+    float2* csl;        // 64 running log2 decays (value, remainder); for the wide chain decays from the chunk's start and to its end
+    float* o;           // (T, Hv * d_v) fp32 outputs before the norm; NULL: there is no norm, or the chain does it
 };
 
-// TMA descriptors of one call: boxes of 64 values x 64 rows of q and k, of a slice x 64 rows of v.
+// TMA descriptors of one call: boxes of 64 values x 64 rows of q and k, of a slice x 64 rows of v and (for the wide chain, where there is a gate) of z.
 struct GdrMaps {
-    CUtensorMap q, k, v;
+    CUtensorMap q, k, v, z;
 };
 
 // Chunks side by side, then a chain over the chunks of each sequence; `slice` = values of a head per block of the chain (16 or 32).
+// slice = d_v: the wide chain.
 cudaError_t launch_gdr_chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_k, int d_v, int slice, cudaStream_t st);
+cudaError_t launch_gdr_chain_wide(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_k, int d_v, cudaStream_t st);
 
 struct GdrStepArgs {
     GdrLayerDev L;

@@ -100,7 +100,7 @@ __device__ __forceinline__ float4 small_product(const float* a, const float* b, 
     return r;
 }
 
-template <int DK>
+template <int DK, bool kWide>
 __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps) {
     extern __shared__ __align__(1024) unsigned char s_raw[];
     PrepSmem<DK>& sm = *reinterpret_cast<PrepSmem<DK>*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
@@ -145,9 +145,10 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         const float hi = (float)sum;
         sm.csl[tid] = make_float2(hi, (float)(sum - hi));
         sm.beta[tid] = beta;
-        ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = sm.csl[tid];
+        if (!kWide) ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = sm.csl[tid];
     }
     __syncthreads();
+    if (kWide && tid < Q) ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = make_float2(ex2(sm.csl[tid].x), ex2(log2_between(sm.csl[tid], sm.csl[Q - 1])));
     const uint32_t tmem = sm.tmem_base;
     const bool in_ok = mbar_wait_bounded(&sm.bar_tma, 0u);
     if (in_ok && tid == 0) {
@@ -255,6 +256,49 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     }
     __syncthreads();
     const float (*M)[kPitch] = reinterpret_cast<const float (*)[kPitch]>(sm.kq);
+    if (kWide) {
+        // Rows of 64 values: T in three parts, M T diag(beta).  A thread takes eight columns of rows lane and lane + 32; columns u and 7 - u, so that every warp has as
+        // much of the triangle.
+        unsigned char* to_T = ws.T + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideTBytes;
+        unsigned char* to_M = ws.M + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideMBytes;
+#pragma unroll 1
+        for (int n = 0; n < 4; ++n) {
+            const int u = n & 1 ? 7 - warp : warp, i = lane + 32 * (n >> 1), c = 8 * u;
+            const uint32_t to = (uint32_t)i * 128 + (uint32_t)((u ^ (i & 7)) * 16);
+            float b[8];
+            *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&sm.beta[c]);
+            *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&sm.beta[c + 4]);
+            uint4 t[3], m;
+            uint32_t *th = &t[0].x, *tm = &t[1].x, *tl = &t[2].x, *mm = &m.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 x = *reinterpret_cast<const float2*>(&sm.A[i][c + 2 * e]);
+                split3(c + 2 * e <= i ? x.x * b[2 * e] : 0.f, c + 2 * e + 1 <= i ? x.y * b[2 * e + 1] : 0.f, th[e], tm[e], tl[e]);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + k * 8192 + to) = t[k];
+            u64 acc[4] = {0ull, 0ull, 0ull, 0ull};
+            for (int k = c; k < 32 + 32 * (n >> 1); k += 4) {   // M is zero behind the diagonal, T ahead of column c
+                const float4 x = *reinterpret_cast<const float4*>(&M[i][k]);
+                const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const ulonglong2 y0 = *reinterpret_cast<const ulonglong2*>(&sm.A[k + j][c]), y1 = *reinterpret_cast<const ulonglong2*>(&sm.A[k + j][c + 4]);
+                    const u64 d = pk(xs[j], xs[j]);
+                    acc[0] = fma2(d, y0.x, acc[0]); acc[1] = fma2(d, y0.y, acc[1]);
+                    acc[2] = fma2(d, y1.x, acc[2]); acc[3] = fma2(d, y1.y, acc[3]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x, y;
+                unpk(acc[e], x, y);
+                mm[e] = pack_bf(x * b[2 * e], y * b[2 * e + 1]);
+            }
+            *reinterpret_cast<uint4*>(to_M + to) = m;
+        }
+        return;
+    }
     unsigned char* to_T = ws.T + ((size_t)cidx * p.L.n_v_heads + head) * kTBytes + lane * 16;
     unsigned char* to_M = ws.M + ((size_t)cidx * p.L.n_v_heads + head) * kMBytes + lane * 16;
     for (int n = warp; n < kBlocks; n += kPrepThreads / 32) {
@@ -752,12 +796,19 @@ cudaError_t chain(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& 
     return launch_pdl(gdr_chain<DK, DVS, STAGES>, dim3(d_v / DVS, p.L.n_v_heads, p.n_seq), kChainThreads, smem, st, p, ws, maps, d_v);
 }
 
+template <int DK, bool kWide>
+cudaError_t prepare(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, cudaStream_t st) {
+    constexpr int smem = sizeof(PrepSmem<DK>) + 1024;
+    const cudaError_t e = allow_smem<gdr_chunk_prepare<DK, kWide>>(smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(gdr_chunk_prepare<DK, kWide>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kPrepThreads, smem, st, p, ws, maps);
+}
+
 template <int DK>
 cudaError_t chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_v, int slice, cudaStream_t st) {
-    constexpr int smem = sizeof(PrepSmem<DK>) + 1024;
-    cudaError_t e = allow_smem<gdr_chunk_prepare<DK>>(smem);
+    cudaError_t e = slice == d_v ? prepare<DK, true>(p, ws, maps, st) : prepare<DK, false>(p, ws, maps, st);
     if (e != cudaSuccess) return e;
-    if ((e = launch_pdl(gdr_chunk_prepare<DK>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kPrepThreads, smem, st, p, ws, maps)) != cudaSuccess) return e;
+    if (slice == d_v) return launch_gdr_chain_wide(p, ws, maps, DK, d_v, st);
     e = slice == 16 ? chain<DK, 16, 3>(p, ws, maps, d_v, st) : chain<DK, 32, 2>(p, ws, maps, d_v, st);
     if (e != cudaSuccess || !ws.o) return e;
     return launch_pdl(d_v == 128 ? gdr_norm_gate<128> : gdr_norm_gate<64>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kNormThreads, 0, st, p, ws.o);

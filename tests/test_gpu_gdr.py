@@ -138,28 +138,43 @@ def test_encode_matches_the_statement(act, hk, hv, dk, dv, lens, init):
     p.check_out(out, w_out, o, size, size64 if is_chunked(p, lens) else None)
 
 
+# As many heads as make the library take a head per block (see plan_gdr in csrc/api.cu).
+MANY = [(20, 20, 128, 128), (7, 21, 64, 128), (5, 40, 128, 64), (38, 38, 64, 64)]
+
+
+@pytest.mark.parametrize("hk,hv,dk,dv", MANY)
+@pytest.mark.parametrize("lens,init", [([40], False), ([64], True), ([200], True), ([1, 2, 0, 63, 64, 65, 130], True)])
+def test_encode_of_many_heads_matches_the_statement(hk, hv, dk, dv, lens, init):
+    p = Problem(sum(lens), hk, hv, dk, dv, gate=init, norm=dk == dv, seed=sum(lens) + hv)
+    cu, h0, out, states = run_encode(p, lens, init, offsets=len(lens) > 1)
+    w_out, w_states, o, size, size64 = gdr.encode(**p.args(), cu=cu, S0=h0, sizes=True)
+    check_states(states, w_states)
+    p.check_out(out, w_out, o, size, size64)
+
+
 @pytest.mark.parametrize("gate", [False, True])
 @pytest.mark.parametrize("norm", [False, True])
-@pytest.mark.parametrize("n", [9, 150])
-def test_encode_with_and_without_norm_and_gate(gate, norm, n):
-    p = Problem(n, 1, 2, gate=gate, norm=norm, seed=4)
+@pytest.mark.parametrize("n,hv", [(9, 2), (150, 2), (150, 24)])
+def test_encode_with_and_without_norm_and_gate(gate, norm, n, hv):
+    p = Problem(n, 1, hv, gate=gate, norm=norm, seed=4)
     cu, h0, out, states = run_encode(p, [n], True, offsets=False)
     w_out, w_states, o, size, size64 = gdr.encode(**p.args(), cu=cu, S0=h0, sizes=True)
     check_states(states, w_states)
     p.check_out(out, w_out, o, size, size64 if is_chunked(p, [n]) else None)
 
 
-@pytest.mark.parametrize("lens", [[5, 9, 3], [100, 1, 0, 70, 200]])
-def test_encode_in_place_equals_slot_to_slot(lens):
-    a = run_encode(Problem(sum(lens), seed=5), lens, True)
-    b = run_encode(Problem(sum(lens), seed=5), lens, True, in_place=True)
+@pytest.mark.parametrize("lens,hv", [([5, 9, 3], 4), ([100, 1, 70], 4), ([100, 1, 0, 70, 200], 6)])
+def test_encode_in_place_equals_slot_to_slot(lens, hv):
+    a = run_encode(Problem(sum(lens), hv=hv, seed=5), lens, True)
+    b = run_encode(Problem(sum(lens), hv=hv, seed=5), lens, True, in_place=True)
     assert torch.equal(a[2].view(torch.int16), b[2].view(torch.int16)) and torch.equal(a[3], b[3])
 
 
-def test_encode_with_raw_gates_and_keys_of_other_sizes():
+@pytest.mark.parametrize("hv", [2, 20])
+def test_encode_with_raw_gates_and_keys_of_other_sizes(hv):
     """Step sizes and strengths as given, zero among them; keys twice and a hundredth of unit length with strengths that fit."""
     for scale, cap in ((2.0, 0.4), (0.01, 1.0)):
-        p = Problem(140, 2, 2, raw=True, seed=6)
+        p = Problem(140, 2, hv, raw=True, seed=6)
         p.np["k"] = gen.round_to_act((p.np["k"] * scale).astype(np.float32), "bf16")
         p.np["beta"] = gen.round_to_act((p.np["beta"] * cap).astype(np.float32), "bf16")
         p.np["dt"][::3] = 0
@@ -171,9 +186,9 @@ def test_encode_with_raw_gates_and_keys_of_other_sizes():
         p.check_out(out, w_out, o, size, size64)
 
 
-@pytest.mark.parametrize("n", [10, 130])
-def test_nothing_written_and_nothing_decayed_leaves_the_state_as_it_was(n):
-    p = Problem(n, 1, 2, raw=True, seed=7)
+@pytest.mark.parametrize("n,hv", [(10, 2), (130, 2), (130, 20)])
+def test_nothing_written_and_nothing_decayed_leaves_the_state_as_it_was(n, hv):
+    p = Problem(n, 1, hv, raw=True, seed=7)
     p.np["dt"][:] = 0
     p.np["beta"][:] = 0
     p.upload()
@@ -181,10 +196,10 @@ def test_nothing_written_and_nothing_decayed_leaves_the_state_as_it_was(n):
     assert torch.equal(states, torch.from_numpy(h0).cuda())
 
 
-@pytest.mark.parametrize("n", [20, 150])
-def test_the_same_key_again_and_again(n):
+@pytest.mark.parametrize("n,hv", [(20, 1), (150, 1), (150, 20)])
+def test_the_same_key_again_and_again(n, hv):
     """Identical keys at full strength: the state holds the last value only; the triangle of a chunk is as full as it gets."""
-    p = Problem(n, 1, 1, raw=True, seed=8, gate=False, norm=False)
+    p = Problem(n, 1, hv, raw=True, seed=8, gate=False, norm=False)
     p.np["k"][:] = 0
     p.np["k"][:, 3] = 1
     p.np["beta"][:] = 1
@@ -195,29 +210,29 @@ def test_the_same_key_again_and_again(n):
     p.check_out(out, w_out, o, size, size64 if is_chunked(p, [n]) else None)
 
 
-@pytest.mark.parametrize("n", [24, 200])
-def test_steep_and_absent_decay(n):
+@pytest.mark.parametrize("n,times", [(24, 1), (200, 1), (200, 5)])
+def test_steep_and_absent_decay(n, times):
     """Heads that forget everything at once (their log decays sum to -10^4 in a chunk), heads that forget nothing."""
-    p = Problem(n, 2, 4, seed=9)
-    p.A[:] = [-3000.0, 0.0, -300.0, -1e-3]
+    p = Problem(n, 2, 4 * times, seed=9)
+    p.A[:] = [-3000.0, 0.0, -300.0, -1e-3] * times
     p.np["dt"][:] = gen.round_to_act(np.random.default_rng(1).uniform(-3, 8, size=p.np["dt"].shape).astype(np.float32), "bf16")
     p.upload()
     cu, h0, out, states = run_encode(p, [n], True)
     w_out, w_states, o, size, size64 = gdr.encode(**p.args(), cu=cu, S0=h0, sizes=True)
-    got, want = (np.asarray(x).reshape(4, 128, 128) for x in (states[0].double().cpu().numpy(), w_states[0]))
-    for j in range(4):   # per head: their sizes differ
+    got, want = (np.asarray(x).reshape(-1, 128, 128) for x in (states[0].double().cpu().numpy(), w_states[0]))
+    for j in range(4 * times):   # per head: their sizes differ
         check_states(torch.from_numpy(got[j]), want[j])
     p.check_out(out, w_out, o, size, size64 if is_chunked(p, [n]) else None)
 
 
-@pytest.mark.parametrize("lens", [[3, 4, 5], [70, 80, 90]])
-def test_values_of_other_sequences_and_of_rows_behind_them_do_not_matter(lens):
+@pytest.mark.parametrize("lens,hv", [([3, 4, 5], 4), ([70, 80, 90], 4), ([70, 80, 90], 8)])
+def test_values_of_other_sequences_and_of_rows_behind_them_do_not_matter(lens, hv):
     """NaN in one sequence's rows and in the rows that belong to none leave the other sequences as they are; those rows' outputs stay unwritten."""
     T = sum(lens) + 7
     cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
     res = []
     for spoil in (False, True):
-        p = Problem(T, seed=10)
+        p = Problem(T, hv=hv, seed=10)
         if spoil:
             for n in ("q", "k", "v", "z", "dt", "beta"):
                 p.np[n][cu[1]:cu[2]] = np.nan
@@ -232,9 +247,9 @@ def test_values_of_other_sequences_and_of_rows_behind_them_do_not_matter(lens):
         assert torch.equal(res[0][0][cu[s]:cu[s + 1]], res[1][0][cu[s]:cu[s + 1]]) and torch.equal(res[0][1][s], res[1][1][s])
 
 
-@pytest.mark.parametrize("lens", [[3, 4], [70, 80]])
-def test_bad_slots_and_offsets_are_flagged_not_followed(lens):
-    p = Problem(sum(lens), seed=12)
+@pytest.mark.parametrize("lens,hv", [([3, 4], 4), ([70, 80], 4), ([70, 80], 10)])
+def test_bad_slots_and_offsets_are_flagged_not_followed(lens, hv):
+    p = Problem(sum(lens), hv=hv, seed=12)
     cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
     ws = p.workspace(2, max(lens))
     for final, offsets, init, bit, good in (([0, 9], cu, None, md.MDRAFT_DEV_BAD_SLOT, 0), ([0, 1], cu, [5, -1], md.MDRAFT_DEV_BAD_SLOT, 1),
@@ -250,9 +265,10 @@ def test_bad_slots_and_offsets_are_flagged_not_followed(lens):
         assert not bool((cache.ssm[0, good] == 5.0).all()) and bool((cache.ssm[0, 1 - good] == 5.0).all()) and bool((cache.ssm[0, 2] == 5.0).all())
 
 
-def test_overlapping_sequences_stay_inside_the_workspace():
+@pytest.mark.parametrize("hv", [4, 20])
+def test_overlapping_sequences_stay_inside_the_workspace(hv):
     T = 300
-    p = Problem(T, seed=13)
+    p = Problem(T, hv=hv, seed=13)
     need = md.mdraft_gdr_prefill_workspace_bytes(p.layer, T, 3, T)
     ws = torch.full((2 * need + 256,), 77, dtype=torch.uint8, device="cuda")
     cache, status, out = p.cache(3), torch.zeros(1, dtype=torch.int32, device="cuda"), p.out()
@@ -452,7 +468,7 @@ def test_on_another_stream_and_replayed_from_a_graph():
 def test_calls_in_a_row_on_one_workspace():
     """Encodes of different shapes one behind another without a wait, sharing a workspace, equal the same calls alone."""
     ps = [(Problem(n, hk, hv, dk, dv, seed=40 + n), lens) for n, hk, hv, dk, dv, lens in
-          ((300, 2, 4, 128, 128, [300]), (260, 1, 3, 64, 128, [130, 130]), (90, 2, 2, 128, 64, [9, 81]), (500, 2, 4, 128, 128, [500]), (24, 1, 1, 128, 128, [8, 16]))]
+          ((300, 2, 4, 128, 128, [300]), (260, 1, 3, 64, 128, [130, 130]), (200, 2, 20, 128, 128, [200]), (70, 3, 21, 64, 64, [33, 37]), (90, 2, 2, 128, 64, [9, 81]), (500, 2, 4, 128, 128, [500]), (24, 1, 1, 128, 128, [8, 16]))]
     alone = [run_encode(p, lens, False)[2:] for p, lens in ps]
     need = max(md.mdraft_gdr_prefill_workspace_bytes(p.layer, p.rows, len(lens), max(lens)) for p, lens in ps)
     ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
