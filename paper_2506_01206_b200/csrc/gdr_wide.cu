@@ -29,6 +29,7 @@ constexpr int Q = kGdrQ;
 constexpr int kStateWarps = 16;                                     // four for each 32 lanes of tensor memory, which split the columns
 constexpr int kOutWarp = kStateWarps, kMmaWarp = kOutWarp + 4, kCopyWarp = kMmaWarp + 1, kGateWarp = kMmaWarp + 2;
 constexpr int kWideThreads = 32 * (kGateWarp + 1), kStages = 2;
+constexpr int kMaxSorted = 512;   // sequences of a call that are taken in order of their length (a block ranks them all for itself)
 constexpr int kBarLanes = 1, kBarRows = 5;   // named barriers: 1 to 4, the state warps of the same 32 lanes; 5, the output warps
 
 template <int DK, int DV>
@@ -46,7 +47,7 @@ struct WideSmem {
     float eo[Q];                 // decay from the chunk's start times scale, for the output warps (which may fall behind the stages)
     float o[Q][DV + 4];          // outputs on their way from a lane per value to a row per warp
     uint64_t full[kStages], done[kStages];                   // copies of a stage, all products that read it
-    uint64_t state, r, w, free_o;                            // operands are in tensor memory, output accumulators have been read
+    uint64_t state[2], r[2], w[2], free_o;                   // operands are in tensor memory (in two portions), output accumulators have been read
     uint64_t mma1, mma2, out, last;                          // products
     uint64_t z_full, z_free;
     uint32_t tmem_base;
@@ -65,14 +66,14 @@ __device__ __forceinline__ bool elect_one() {
 // Two neighbours as three bf16 values each.  The first is rounded (the outputs take it alone), the others are truncated: the remainders are exact, and 8 + 8 + 8
 // bits hold all 24 of a fp32 value.
 __device__ __forceinline__ uint32_t leading_halves(u64 v) { return __byte_perm((uint32_t)v, (uint32_t)(v >> 32), 0x7632); }
-__device__ __forceinline__ void split3(u64 v, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+__device__ __forceinline__ uint32_t split_first(u64& v) {   // leaves the remainder
     float a, b;
     unpk(v, a, b);
-    hi = pack_bf(a, b);
+    const uint32_t hi = pack_bf(a, b);
     v = fma2(pk(bf_lo(hi), bf_hi(hi)), pk(-1.f, -1.f), v);
-    mid = leading_halves(v);
-    lo = leading_halves(fma2(v & 0xffff0000ffff0000ull, pk(-1.f, -1.f), v));
+    return hi;
 }
+__device__ __forceinline__ uint32_t split_last(u64 v) { return leading_halves(fma2(v & 0xffff0000ffff0000ull, pk(-1.f, -1.f), v)); }
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps) {
@@ -84,8 +85,26 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
     extern __shared__ __align__(1024) unsigned char s_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int head = blockIdx.x, seq = blockIdx.y;
+    const int head = blockIdx.x;
     grid_release_dependents();
+    int seq = blockIdx.y;
+    if (p.n_seq > 1 && p.n_seq <= kMaxSorted) {   // the longest sequences first: the blocks that start last are to be the short ones
+        int* const pick = reinterpret_cast<int*>(&sm);
+        if (tid < p.n_seq) {
+            int a, mine, b, other;
+            bool bad_a, bad_b;
+            seq_span(p.cu, p.n_seq, p.T, tid, a, mine, bad_a);
+            int rank = 0;
+            for (int i = 0; i < p.n_seq; ++i) {
+                seq_span(p.cu, p.n_seq, p.T, i, b, other, bad_b);
+                rank += other > mine || (other == mine && i < tid);
+            }
+            if (rank == (int)blockIdx.y) *pick = tid;
+        }
+        __syncthreads();
+        seq = *pick;
+        __syncthreads();
+    }
     int first, nck, s0, len;
     bool bad;
     seq_chunks(p.cu, p.n_seq, p.T, Q, p.n_chunks_bound, seq, first, nck);
@@ -101,7 +120,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
     if (tid == 0) {
 #pragma unroll
         for (int i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.done[i], 1); }
-        mbar_init(&sm.state, kStateWarps); mbar_init(&sm.r, kStateWarps); mbar_init(&sm.w, kStateWarps); mbar_init(&sm.free_o, 4);   // a lane of every warp
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { mbar_init(&sm.state[i], kStateWarps); mbar_init(&sm.r[i], kStateWarps); mbar_init(&sm.w[i], kStateWarps); }   // a lane of every warp
+        mbar_init(&sm.free_o, 4);
         mbar_init(&sm.mma1, 1); mbar_init(&sm.mma2, 1); mbar_init(&sm.out, 1); mbar_init(&sm.last, 1);
         mbar_init(&sm.z_full, 1); mbar_init(&sm.z_free, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -133,52 +154,89 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
             if (islot >= 0 && rows_here) v = *reinterpret_cast<const float4*>(p.pool.ssm + (size_t)islot * p.pool.ssm_slot_stride + at + i);
             S[i / 2] = pk(v.x, v.y); S[i / 2 + 1] = pk(v.z, v.w);
         }
-        auto put_state = [&] {
-            if (rows_here) {
+        auto put_state = [&] {   // every second step of d_k is handed over first
 #pragma unroll
-                for (int i = 0; i < C; i += 16) {
+            for (int i = 0; i < C; i += 16) {
+                if (rows_here) {
                     uint32_t a[3][8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) split3(S[i / 2 + j], a[0][j], a[1][j], a[2][j]);
+                    for (int j = 0; j < 8; ++j) {
+                        u64 v = S[i / 2 + j];
+                        a[0][j] = split_first(v);
+                        a[1][j] = leading_halves(v);
+                        a[2][j] = split_last(v);
+                    }
 #pragma unroll
                     for (int k = 0; k < 3; ++k) tmem_st8(tmem + lanes + kS + k * (DK / 2) + part * (C / 2) + i / 2, a[k]);
+                    tmem_wait_st();
                 }
-                tmem_wait_st();
+                arrive(&sm.state[i / 16]);
             }
-            arrive(&sm.state);
         };
         if (nck > 0) put_state();
         for (int c = 0; c < nck; ++c) {
             WideStage<DK, DV>& s = sm.stage[c % kStages];
-            const float2* ef = s.ef + 16 * part;   // of the 16 tokens that the thread takes
-            const int rows = len - c * Q, mine = rows - 16 * part;
+            // The thread takes eight tokens of the first half of the chunk and the eight that lie 32 further on, and hands them over in that order.
+            const float2* ef = s.ef + 8 * part;
+            const int rows = len - c * Q, mine = rows - 8 * part;
             wait(&sm.full[c % kStages], c / kStages);
             uint32_t vv[8];   // values of two tokens each
             {
-                const unsigned short* vp = reinterpret_cast<const unsigned short*>(&s.v[16 * part][rows_here ? row : 0]);
+                const unsigned short* vp = reinterpret_cast<const unsigned short*>(&s.v[8 * part][rows_here ? row : 0]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) vv[j] = (uint32_t)vp[2 * j * DV] | (uint32_t)vp[(2 * j + 1) * DV] << 16;
+                for (int j = 0; j < 8; ++j) {
+                    const int t = 2 * j + (j < 4 ? 0 : 24);
+                    vv[j] = (uint32_t)vp[t * DV] | (uint32_t)vp[(t + 1) * DV] << 16;
+                }
             }
             wait(&sm.mma1, c);
             tc_fence_after();
-            if (rows_here && ok) {
-                float v[16];
-                tmem_ld16(tmem + lanes + kD1 + 16 * part, v);
-                if (mine < 16) {   // tokens past the chunk's end may hold anything: replaced, not scaled
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = j < mine ? v[j] : 0.f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) vv[j] &= (2 * j < mine ? 0xffffu : 0u) | (2 * j + 1 < mine ? 0xffff0000u : 0u);
+            float v[2][8];
+            auto load_d1 = [&] {
+                if (rows_here && ok) {
+                    tmem_ld8_begin(tmem + lanes + kD1 + 8 * part, v[0]);
+                    tmem_ld8_begin(tmem + lanes + kD1 + 32 + 8 * part, v[1]);
+                    tmem_ld_end(v[0], v[1]);
                 }
-                uint32_t a[3][8];
+            };
+            auto hand_over = [&](const u64 (&x)[4], uint32_t hi, uint32_t mid, uint32_t lo, int hand, uint64_t* bar) {
+                if (rows_here && ok) {
+                    uint32_t a[3][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        u64 y = x[j];
+                        a[0][j] = split_first(y);
+                        a[1][j] = leading_halves(y);
+                        a[2][j] = split_last(y);
+                    }
+                    const uint32_t to = tmem + lanes + 16 * hand + 4 * part;
+                    tmem_st4(to + hi, a[0]);
+                    tmem_st4(to + mid, a[1]);
+                    tmem_st4(to + lo, a[2]);
+                    tmem_wait_st();
+                }
+                arrive(bar);
+            };
+            load_d1();
+            if (rows < Q && rows_here && ok) {   // tokens past the chunk's end may hold anything: replaced, not scaled
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float4 e = *reinterpret_cast<const float4*>(&ef[2 * j]);   // (e, f) of two tokens
-                    split3(fma2(pk(-e.x, -e.z), pk(v[2 * j], v[2 * j + 1]), pk(bf_lo(vv[j]), bf_hi(vv[j]))), a[0][j], a[1][j], a[2][j]);
+                    v[0][j] = j < mine ? v[0][j] : 0.f;
+                    v[1][j] = 32 + j < mine ? v[1][j] : 0.f;
+                    const int t = 2 * j + (j < 4 ? 0 : 24);
+                    vv[j] &= (t < mine ? 0xffffu : 0u) | (t + 1 < mine ? 0xffff0000u : 0u);
                 }
+            }
 #pragma unroll
-                for (int k = 0; k < 3; ++k) tmem_st8(tmem + lanes + kR + k * 32 + 8 * part, a[k]);
-                tmem_wait_st();
+            for (int hand = 0; hand < 2; ++hand) {
+                u64 x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 e = *reinterpret_cast<const float4*>(&ef[32 * hand + 2 * j]);   // (e, f) of two tokens
+                    const uint32_t w = vv[4 * hand + j];
+                    x[j] = fma2(pk(-e.x, -e.z), pk(v[hand][2 * j], v[hand][2 * j + 1]), pk(bf_lo(w), bf_hi(w)));
+                }
+                hand_over(x, kR, kR + 32, kR + 64, hand, &sm.r[hand]);
             }
             if (rows < Q) {   // keys of other sequences, which may be anything, would meet zeros in the update
                 for (int i = tid; i < (Q - rows) * (DK / 8); i += 32 * kStateWarps) {
@@ -187,23 +245,19 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                 }
                 fence_async_smem();
             }
-            arrive(&sm.r);
             wait(&sm.mma2, c);
             tc_fence_after();
-            if (rows_here && ok) {
-                float v[16];
-                tmem_ld16(tmem + lanes + kD1 + 16 * part, v);
-                uint32_t a[3][8];
+            load_d1();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float4 e = *reinterpret_cast<const float4*>(&ef[2 * j]);
-                    split3(mul2(pk(e.y, e.w), pk(v[2 * j], v[2 * j + 1])), a[0][j], a[1][j], a[2][j]);
+            for (int hand = 0; hand < 2; ++hand) {
+                u64 x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 e = *reinterpret_cast<const float4*>(&ef[32 * hand + 2 * j]);
+                    x[j] = mul2(pk(e.y, e.w), pk(v[hand][2 * j], v[hand][2 * j + 1]));
                 }
-#pragma unroll
-                for (int k = 0; k < 3; ++k) tmem_st8(tmem + lanes + kW[k] + 8 * part, a[k]);
-                tmem_wait_st();
+                hand_over(x, kW[0], kW[1], kW[2], hand, &sm.w[hand]);
             }
-            arrive(&sm.w);
             const float all = s.ef[Q - 1].x;
             wait(&sm.done[c % kStages], c / kStages);
             tc_fence_after();
@@ -308,17 +362,30 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
             const uint64_t dK = operand_desc_sw128(smem_u32(s.k)), dQ = operand_desc_sw128(smem_u32(s.q)), dT = operand_desc_sw128(smem_u32(s.T)),
                            dM = operand_desc_sw128(smem_u32(s.M)), dKc = operand_desc_sw128_mn(smem_u32(s.k), 8192, 1024);
             wait(&sm.full[c % kStages], c / kStages);
-            wait(&sm.state, c);
-            tc_fence_after();
-            if (ok && elect_one()) {
+            constexpr int kHands = DK / 64;   // portions in which the state comes
+            auto keys = [&](int hand) {
 #pragma unroll
                 for (int part = 2; part >= 0; --part)
 #pragma unroll
-                    for (int k = 0; k < DK / 16; ++k)
-                        mma_bf16_ts(tmem + kD1, tmem + kS + part * (DK / 2) + k * 8, dK + (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4), idTok, part < 2 || k > 0);
-                mma_commit(&sm.mma1);
+                    for (int k = hand; k < DK / 16; k += kHands)
+                        mma_bf16_ts(tmem + kD1, tmem + kS + part * (DK / 2) + k * 8, dK + (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4), idTok, hand > 0 || part < 2 || k > 0);
+            };
+            auto tokens = [&](uint32_t to, int part, uint64_t d, int tile, int hand, bool more) {   // over half the tokens
+#pragma unroll
+                for (int k = 2 * hand; k < 2 * hand + 2; ++k)
+                    mma_bf16_ts(tmem + to, tmem + kR + part * 32 + k * 8, d + (uint64_t)((tile * 8192 + k * 32) >> 4), idTok, more || k > 2 * hand);
+            };
+            // D1 = S K^T
+#pragma unroll
+            for (int hand = 0; hand < kHands; ++hand) {
+                wait(&sm.state[hand], c);
+                tc_fence_after();
+                if (ok && elect_one()) {
+                    keys(hand);
+                    if (hand == kHands - 1) mma_commit(&sm.mma1);
+                }
+                __syncwarp();
             }
-            __syncwarp();
             if (c > 0) {
                 wait(&sm.free_o, c - 1);   // the outputs ahead have left their accumulators
                 tc_fence_after();
@@ -329,33 +396,44 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                     mma_bf16_ts(tmem + kDQ, tmem + kS + k * 8, dQ + (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4), idTok, k > 0);
             }
             __syncwarp();
-            wait(&sm.r, c);
-            tc_fence_after();
-            if (ok && elect_one()) {
-                constexpr int of_R[6] = {2, 0, 1, 1, 0, 0}, of_T[6] = {0, 2, 1, 0, 1, 0};   // the six products that reach 24 bits, small ones first
+            // X = R T^T: the six products of parts that reach 24 bits, small ones first
 #pragma unroll
-                for (int i = 0; i < 6; ++i)
-#pragma unroll
-                    for (int k = 0; k < Q / 16; ++k)
-                        mma_bf16_ts(tmem + kD1, tmem + kR + of_R[i] * 32 + k * 8, dT + (uint64_t)((of_T[i] * 8192 + k * 32) >> 4), idTok, i > 0 || k > 0);
-                mma_commit(&sm.mma2);
-#pragma unroll
-                for (int part = 1; part >= 0; --part)
-#pragma unroll
-                    for (int k = 0; k < Q / 16; ++k) mma_bf16_ts(tmem + kDO, tmem + kR + part * 32 + k * 8, dM + (uint64_t)(k * 32 >> 4), idTok, part < 1 || k > 0);
-                mma_commit(&sm.out);
+            for (int hand = 0; hand < 2; ++hand) {
+                wait(&sm.r[hand], c);
+                tc_fence_after();
+                if (ok && elect_one()) {
+                    tokens(kD1, 2, dT, 0, hand, hand > 0);
+                    tokens(kD1, 0, dT, 2, hand, true);
+                    tokens(kD1, 1, dT, 1, hand, true);
+                    tokens(kD1, 1, dT, 0, hand, true);
+                    tokens(kD1, 0, dT, 1, hand, true);
+                    tokens(kD1, 0, dT, 0, hand, true);
+                    if (hand == 1) {
+                        mma_commit(&sm.mma2);
+                        tokens(kDO, 1, dM, 0, 0, false);
+                        tokens(kDO, 0, dM, 0, 0, true);
+                        tokens(kDO, 1, dM, 0, 1, true);
+                        tokens(kDO, 0, dM, 0, 1, true);
+                        mma_commit(&sm.out);
+                    }
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            wait(&sm.w, c);
-            tc_fence_after();
-            if (ok && elect_one()) {
+            // W K
 #pragma unroll
-                for (int part = 2; part >= 0; --part)
+            for (int hand = 0; hand < 2; ++hand) {
+                wait(&sm.w[hand], c);
+                tc_fence_after();
+                if (ok && elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < Q / 16; ++k) mma_bf16_ts(tmem + kD3, tmem + kW[part] + k * 8, dKc + (uint64_t)(k * 2048 >> 4), idUpd, part < 2 || k > 0);
-                mma_commit(&sm.done[c % kStages]);
+                    for (int part = 2; part >= 0; --part)
+#pragma unroll
+                        for (int k = 2 * hand; k < 2 * hand + 2; ++k)
+                            mma_bf16_ts(tmem + kD3, tmem + kW[part] + k * 8, dKc + (uint64_t)(k * 2048 >> 4), idUpd, hand > 0 || part < 2 || k > 0);
+                    if (hand == 1) mma_commit(&sm.done[c % kStages]);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
     } else if (warp == kCopyWarp) {
         // ---------------------------------------------------------------- copies
@@ -382,6 +460,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
         }
     } else if (warp == kGateWarp && p.io.z) {
         for (int c = 0; c < nck; ++c) {
+            // one buffer, asked for late: the rows are brought as far as L2 ahead of that
+            if (lane == 0 && c + 1 < nck)
+                asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(&maps.z)), "r"(head * DV), "r"(s0 + (c + 1) * Q) : "memory");
             if (c > 0) wait(&sm.z_free, c - 1);
             if (!ok) break;
             if (lane == 0) {
