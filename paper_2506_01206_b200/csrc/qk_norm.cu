@@ -4,10 +4,10 @@
 //     (y_a, y_b) <- rot_scale (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position freqs[i],
 //     (a, b) = (i, i + rot/2) or (2i, 2i + 1) for i < rot/2
 //
-// A head is 8 values (16 or 32 bytes) per lane of a lane group (2 to 32 lanes), so the sum of squares takes one to five shuffles and a
-// rotation by halves finds its other half in another lane of the group.  The turns of a row (position times frequency, reduced
+// A head is 8 values per lane of a lane group (4 to 32 lanes), so the sum of squares takes two to five shuffles; a rotation by halves has four values of
+// either half in a lane (two loads of 8 or 16 bytes), so that it takes none.  The turns of a row (position times frequency, reduced
 // to [-1/2, 1/2] turns in 64 bits, as an fp32 product is off by whole radians at positions of a million) are formed once and shared by its heads
-// through shared memory.  A block takes as many rows as give each of its lane groups up to kItems heads, all loaded before the first is used.
+// through shared memory.  A block works through passes of rows and has the next one's loads in flight meanwhile.
 #include "common.cuh"
 #include "qk_norm.cuh"
 
@@ -15,131 +15,166 @@ namespace mdraft {
 
 namespace {
 
-constexpr int kThreads = 256, kItems = 4, kMaxRows = 16;
+template <typename T> constexpr int kItemsOf = 8 / sizeof(T);   // heads a lane group has in flight: 64 bytes a lane
+constexpr int kThreads = 256, kMaxThreads = 512;       // of a block as a rule, and where the heads of a row ask for more
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+// Two times four values as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p, int to_b) {
+        a = *reinterpret_cast<const float4*>(p);
+        b = *reinterpret_cast<const float4*>(p + to_b);
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
+    __device__ __forceinline__ void widen(float (&v)[8]) const { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w; }
+    __device__ static __forceinline__ void store(float* p, int to_b, const float (&v)[8]) {
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(p + to_b) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+};
+template <> struct Raw<__nv_bfloat16> {
+    uint2 a, b;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int to_b) {
+        a = *reinterpret_cast<const uint2*>(p);
+        b = *reinterpret_cast<const uint2*>(p + to_b);
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const {
+        const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    __device__ static __forceinline__ uint32_t pack(float lo, float hi) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&b);
+    }
+    __device__ static __forceinline__ void store(__nv_bfloat16* p, int to_b, const float (&v)[8]) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
+        *reinterpret_cast<uint2*>(p + to_b) = make_uint2(pack(v[4], v[5]), pack(v[6], v[7]));
+    }
+};
 
-// G lanes per head; `rows_per_block` rows, whose heads (row by row, queries first) the block's lane groups take in turn.
-template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) qk_norm_kernel(const QkNormArgs p, int rows_per_block) {
-    extern __shared__ float2 turns[];   // [row][rot_dim / 2] (cos, sin), times rot_scale
-    constexpr int kGroups = kThreads / G;
+// How the work is cut.  A block takes `heads` heads (a part of a row's where there are more than fit) of `row_lanes` rows side by side, a lane group each: so a
+// group has the same head throughout.  A pass is `items` such steps.
+struct Cut {
+    int heads, row_lanes, items, passes;
+};
+
+// G lanes per head.  A block loads its next pass before it works on the one at hand, and forms the next rows' turns behind it.
+template <typename T, int G, bool kHalf>
+__global__ void __launch_bounds__(kMaxThreads, 2) qk_norm_kernel(const QkNormArgs p, const Cut cut) {
+    extern __shared__ __align__(16) float2 turns[];   // [2][row of the pass][rot_dim / 2, rounded up to 4] (cos, sin), times rot_scale
+    constexpr int kItems = kItemsOf<T>;
     const int tid = threadIdx.x, l = tid % G, group = tid / G;
-    const int row0 = blockIdx.x * rows_per_block, rows = min(rows_per_block, p.rows - row0);
-    const int heads = p.n_q_heads + p.n_k_heads, items = rows * heads, half = p.rot_dim / 2;
-    const bool mine = 8 * l < p.d_head;
-    float x[kItems][8];
-    auto source = [&](int item, bool& key, int64_t& row, int& h) {
-        row = row0 + item / heads;
-        h = item % heads;
-        key = h >= p.n_q_heads;
-        if (key) h -= p.n_q_heads;
+    const int lane_row = group / cut.heads, in_part = group - lane_row * cut.heads, half = p.rot_dim / 2, pitch = (half + 3) & ~3;
+    const int h = blockIdx.y * cut.heads + in_part, per_pass = cut.row_lanes * cut.items;
+    const bool key = h >= p.n_q_heads, mine = lane_row < cut.row_lanes && h < p.n_q_heads + p.n_k_heads && 8 * l < p.d_head;
+    // A rotation by halves takes four values of either half into a lane, so that every pair is in one lane.
+    const bool turned = 8 * l < p.rot_dim;
+    const int at = kHalf && turned ? 4 * l : 8 * l, to_b = kHalf && turned ? half : 4;
+    const int64_t column = mine ? (int64_t)(key ? h - p.n_q_heads : h) * p.d_head + at : 0, ld = key ? p.ldk : p.ldq, ldo = key ? p.ldko : p.ldqo;
+    const T* from = static_cast<const T*>(key ? p.k : p.q) + column;   // lanes without a share of a head read something, and write nothing
+    T* to = static_cast<T*>(key ? p.k_out : p.q_out) + column;
+    if (h >= p.n_q_heads + p.n_k_heads) from = static_cast<const T*>(p.n_q_heads ? p.q : p.k);
+    const int reach = mine ? to_b : 4;
+    const float per_value = p.norm == MDRAFT_NORM_RMS ? 1.0f / (float)p.d_head : 1.0f;
+    float weight[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) weight[e] = 1.0f;
+    if (const float* w = key ? p.k_w : p.q_w; w && mine && p.norm != MDRAFT_NORM_NONE)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) weight[e] = __ldg(w + at + (e < 4 ? e : to_b + e - 4));
+    Raw<T> raw[kItems];
+    auto load = [&](int pass) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int row = pass * per_pass + i * cut.row_lanes + lane_row;
+            if (i < cut.items) raw[i].load(from + (row < p.rows ? row : p.rows - 1) * ld, reach);
+        }
     };
-    for (int first = 0; first < items; first += kGroups * kItems) {   // the same trips for every thread
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int item = first + group + i * kGroups;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-            if (item < items && mine) {
-                bool key; int64_t row; int h;
-                source(item, key, row, h);
-                const T* s = key ? static_cast<const T*>(p.k) + row * p.ldk : static_cast<const T*>(p.q) + row * p.ldq;
-                load8(s + (size_t)h * p.d_head + 8 * l, x[i]);
-            }
+    auto turn = [&](int pass, float2* out) {
+        const int row0 = pass * per_pass, n = min(per_pass, p.rows - row0) * half;
+        for (int i = tid; i < n; i += blockDim.x) {
+            const int r = i / half, c = i - r * half;
+            double t = (double)__ldg(p.positions + row0 + r) * (double)__ldg(p.freqs + c) * 0.15915494309189535;   // in turns
+            t -= rint(t);
+            float sn, cs;
+            sincospif((float)(2.0 * t), &sn, &cs);
+            out[r * pitch + c] = make_float2(cs * p.rot_scale, sn * p.rot_scale);
         }
-        if (first == 0 && half > 0) {
-            for (int i = tid; i < rows * half; i += kThreads) {
-                const int r = i / half, c = i % half;
-                double t = (double)__ldg(p.positions + row0 + r) * (double)__ldg(p.freqs + c) * 0.15915494309189535;   // in turns
-                t -= rint(t);
-                float sn, cs;
-                sincospif((float)(2.0 * t), &sn, &cs);
-                turns[i] = make_float2(cs * p.rot_scale, sn * p.rot_scale);
-            }
-            __syncthreads();
-        }
+    };
+    const int pairs = kHalf ? 4 : (p.rot_dim - 8 * l) / 2;   // of the lane that are turned
+    int pass = blockIdx.x, buffer = 0;
+    load(pass);
+    if (half > 0) {
+        turn(pass, turns);
+        __syncthreads();
+    }
+    for (; pass < cut.passes; pass += gridDim.x, buffer ^= 1) {
+        Raw<T> now[kItems];
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int item = first + group + i * kGroups;
-            bool key; int64_t row; int h;
-            source(min(item, items - 1), key, row, h);   // lanes without a head take part in the shuffles
+        for (int i = 0; i < kItems; ++i) now[i] = raw[i];
+        const int next = pass + gridDim.x;
+        if (next < cut.passes) load(next);
+        const float2* tr = turns + (buffer * per_pass + (mine ? lane_row : 0)) * pitch;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {   // lanes without a head take part in the shuffles
+            if (i >= cut.items) break;
+            const int row = pass * per_pass + i * cut.row_lanes + lane_row;
+            float x[8];
+            now[i].widen(x);
             if (p.norm != MDRAFT_NORM_NONE) {
                 float sq = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq = fmaf(x[i][e], x[i][e], sq);
+                for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
+                if (!mine) sq = 0.f;
 #pragma unroll
                 for (int o = 1; o < G; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                const float f = rsqrtf((p.norm == MDRAFT_NORM_RMS ? sq / (float)p.d_head : sq) + p.eps);
-                const float* w = key ? p.k_w : p.q_w;
-                float wv[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-                if (w && mine) load8(w + 8 * l, wv);
+                const float f = rsqrtf(fmaf(sq, per_value, p.eps));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] *= f * wv[e];
+                for (int e = 0; e < 8; ++e) x[e] *= f * weight[e];
             }
-            const float2* tr = turns + (row - row0) * half;
-            if (p.rot_layout == MDRAFT_ROT_PAIRS) {
+            if (turned) {
+                const float4* t = reinterpret_cast<const float4*>(tr + i * cut.row_lanes * pitch + 4 * l);
+                const float4 t0 = t[0], t1 = t[1];
+                const float c[4] = {t0.x, t0.z, t1.x, t1.z}, sn[4] = {t0.y, t0.w, t1.y, t1.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (8 * l + 2 * e < p.rot_dim) {
-                        const float2 c = tr[4 * l + e];
-                        const float a = x[i][2 * e], b = x[i][2 * e + 1];
-                        x[i][2 * e] = a * c.x - b * c.y;
-                        x[i][2 * e + 1] = b * c.x + a * c.y;
-                    }
-                }
-            } else if (half > 0) {
-                const int m = half / 8;   // lanes per half
-                const bool low = l < m, turned = l < 2 * m;
-                const int src = low ? l + m : (turned ? l - m : l);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float other = __shfl_sync(0xffffffffu, x[i][e], src, G);
-                    if (turned) {
-                        const float2 c = tr[8 * (low ? l : l - m) + e];
-                        x[i][e] = low ? x[i][e] * c.x - other * c.y : x[i][e] * c.x + other * c.y;
+                    float& a = x[kHalf ? e : 2 * e];
+                    float& b = x[kHalf ? e + 4 : 2 * e + 1];
+                    if (e < pairs) {
+                        const float was = a;
+                        a = fmaf(-b, sn[e], was * c[e]);
+                        b = fmaf(was, sn[e], b * c[e]);
                     }
                 }
             }
-            if (item < items && mine) {
-                T* d = key ? static_cast<T*>(p.k_out) + row * p.ldko : static_cast<T*>(p.q_out) + row * p.ldqo;
-                store8(d + (size_t)h * p.d_head + 8 * l, x[i]);
-            }
+            if (mine && row < p.rows) Raw<T>::store(to + row * ldo, to_b, x);
+        }
+        if (half > 0 && next < cut.passes) {
+            turn(next, turns + (buffer ^ 1) * per_pass * pitch);
+            __syncthreads();
         }
     }
 }
 
 template <typename T, int G>
 cudaError_t launch(const QkNormArgs& p, cudaStream_t st) {
-    // Enough rows that every lane group has kItems heads in flight, as long as that leaves two blocks per SM.
     const int heads = p.n_q_heads + p.n_k_heads;
-    int rows = (kThreads / G * kItems) / heads;
-    if (rows > kMaxRows) rows = kMaxRows;
-    while (rows > 1 && (p.rows + rows - 1) / rows < 2 * sm_count()) --rows;
-    if (rows < 1) rows = 1;
-    qk_norm_kernel<T, G><<<(p.rows + rows - 1) / rows, kThreads, (size_t)rows * (p.rot_dim / 2) * sizeof(float2), st>>>(p, rows);
+    Cut cut;
+    cut.heads = heads < kMaxThreads / G ? heads : kMaxThreads / G;
+    cut.row_lanes = kThreads / (cut.heads * G) > 0 ? kThreads / (cut.heads * G) : 1;
+    const int parts = (heads + cut.heads - 1) / cut.heads, threads = (cut.heads * cut.row_lanes * G + 31) / 32 * 32;
+    // Few rows are spread over the SMs, many are taken by as many blocks as fit at once.
+    cut.items = kItemsOf<T>;
+    auto passes = [&] { return (p.rows + cut.row_lanes * cut.items - 1) / (cut.row_lanes * cut.items); };
+    while (cut.items > 1 && passes() * (int64_t)parts < 2 * sm_count()) --cut.items;
+    while (cut.row_lanes > 1 && passes() * (int64_t)parts < 2 * sm_count()) cut.row_lanes /= 2;
+    cut.passes = passes();
+    const int most = (2 * kMaxThreads / threads) * sm_count() / parts;   // resident at once
+    const int blocks = cut.passes < most ? cut.passes : (most > 0 ? most : 1);
+    const size_t smem = 2 * (size_t)(cut.row_lanes * cut.items) * ((p.rot_dim / 2 + 3) & ~3) * sizeof(float2);
+    if (p.rot_layout == MDRAFT_ROT_HALF) qk_norm_kernel<T, G, true><<<dim3(blocks, parts), threads, smem, st>>>(p, cut);
+    else qk_norm_kernel<T, G, false><<<dim3(blocks, parts), threads, smem, st>>>(p, cut);
     return cudaGetLastError();
 }
 
