@@ -46,9 +46,14 @@ constexpr int kPitch = 68;   // floats of a row of A and M
 
 template <int DK>
 struct PrepSmem {
-    static constexpr int kTile = DK / 64 * 128 * 128 > Q * kPitch * 4 ? DK / 64 * 128 * 128 : Q * kPitch * 4;
-    unsigned char kq[kTile];       // [K; Q] rows in boxes of 64 values, 128-byte swizzle  ->  M as fp32
-    float A[Q][kPitch];            // blocks of A, each replaced by its block of the inverse
+    static constexpr int kOperands = DK / 64 * 128 * 128, kMatrices = 2 * Q * kPitch * 4;
+    union {
+        unsigned char kq[kOperands];   // [K; Q] rows in boxes of 64 values, 128-byte swizzle; free once the product is done, then
+        struct {
+            float A[Q][kPitch];        // blocks of A, each replaced by its block of the inverse
+            float M[Q][kPitch];
+        };
+    };
     float Z[32][36];               // product on the way to a block of the inverse
     float2 csl[Q];                 // running log2 decay (value, remainder)
     float u[Q];                    // decay from the first row of a row's block to the row
@@ -123,7 +128,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
             tma_box(sm.kq + h * 16384 + 8192, &maps.q, kcol + 64 * h, ci.t0, &sm.bar_tma);
         }
     }
-    if (warp == 0) { tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
+    if (warp == 3) { tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
     float g = 0.f, beta = 0.f;   // rows past the chunk's end: no decay, nothing written
     if (tid < rows) {
         const size_t t = (size_t)(ci.t0 + tid);
@@ -171,38 +176,49 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     ok = !__syncthreads_or(!ok);   // the decays are visible, the operands are free
     if (ok) {
         tc_fence_after();
-        const bool query = warp >= 2;
-        const int i = tid & 63, rb = i >> 4;
-        float* row = query ? reinterpret_cast<float(*)[kPitch]>(sm.kq)[i] : sm.A[i];
+        const bool query = warp >= 2, upper = lane >= 16;   // rows of the odd 16 x 16 blocks
+        const int i = tid & 63, rb = i >> 4, c0 = 32 * (warp & 1);
+        float* row = query ? sm.M[i] : sm.A[i];
         const float2 mine = sm.csl[i];
         const float f = i < rows ? (query ? p.L.scale : sm.beta[i]) : 0.f, fu = f * sm.u[i];
-        const int last = i < rows ? (query ? i : i - 1) : -1;   // columns up to here count
-        for (int cb = 0; cb < 2 + 2 * (warp & 1); ++cb) {       // blocks that some row of the warp has
-            float v[16];
-            __syncwarp();
-            tmem_ld16(tmem + ((uint32_t)(warp * 32) << 16) + cb * 16, v);
+        const uint32_t t = tmem + ((uint32_t)(warp * 32) << 16);
+        auto off_diagonal = [&](const float (&v)[16], int c) {
 #pragma unroll
             for (int j = 0; j < 16; j += 4) {
-                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (cb < rb) {
-                    const float4 d = *reinterpret_cast<const float4*>(&sm.v[rb][cb * 16 + j]);
-                    w = make_float4(v[j] * (fu * d.x), v[j + 1] * (fu * d.y), v[j + 2] * (fu * d.z), v[j + 3] * (fu * d.w));
-                    if (i >= rows) w = make_float4(0.f, 0.f, 0.f, 0.f);
-                } else if (cb == rb) {
-                    float* e = &w.x;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = cb * 16 + j + k;
-                        e[k] = c <= last ? v[j + k] * f * ex2(log2_between(sm.csl[c], mine)) : 0.f;   // replaced, not scaled: what is masked may be anything
-                    }
-                }
-                *reinterpret_cast<float4*>(row + cb * 16 + j) = w;
+                const float4 d = *reinterpret_cast<const float4*>(&sm.v[rb][c + j]);
+                float4 w = make_float4(v[j] * (fu * d.x), v[j + 1] * (fu * d.y), v[j + 2] * (fu * d.z), v[j + 3] * (fu * d.w));
+                if (i >= rows) w = make_float4(0.f, 0.f, 0.f, 0.f);   // replaced, not scaled: what is masked may be anything
+                *reinterpret_cast<float4*>(row + c + j) = w;
             }
+        };
+        float a[16], b[16];
+        tmem_ld16(t + c0, a);
+        tmem_ld16(t + c0 + 16, b);
+        if (upper) off_diagonal(a, c0);
+        else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(row + c0 + 16 + j) = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        __syncwarp();
+        const int last = i < rows ? i - 16 * rb - (query ? 0 : 1) : -1;   // columns of the diagonal block up to here count
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            float4 w;
+            float* e = &w.x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = j + k <= last ? (upper ? b[j + k] : a[j + k]) * f * ex2(log2_between(sm.csl[16 * rb + j + k], mine)) : 0.f;
+            *reinterpret_cast<float4*>(row + 16 * rb + j) = w;
+        }
+        if (c0 > 0) {
+            tmem_ld16(t, a);
+            tmem_ld16(t + 16, b);
+            off_diagonal(a, 0);
+            off_diagonal(b, 16);
         }
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 0) tmem_free(tmem, 64);
+    if (warp == 3) tmem_free(tmem, 64);
     if (!ok) {
         if (tid == 0) {
             flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
@@ -255,47 +271,55 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         *reinterpret_cast<float4*>(&sm.A[48 + r][c]) = make_float4(-z1.x, -z1.y, -z1.z, -z1.w);
     }
     __syncthreads();
-    const float (*M)[kPitch] = reinterpret_cast<const float (*)[kPitch]>(sm.kq);
     if (kWide) {
         // Rows of 64 values: T in three parts, M T diag(beta).  A thread takes eight columns of rows lane and lane + 32; columns u and 7 - u, so that every warp has as
         // much of the triangle.
         unsigned char* to_T = ws.T + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideTBytes;
         unsigned char* to_M = ws.M + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideMBytes;
 #pragma unroll 1
-        for (int n = 0; n < 4; ++n) {
-            const int u = n & 1 ? 7 - warp : warp, i = lane + 32 * (n >> 1), c = 8 * u;
-            const uint32_t to = (uint32_t)i * 128 + (uint32_t)((u ^ (i & 7)) * 16);
+        for (int n = 0; n < 2; ++n) {
+            const int u = n ? 7 - warp : warp, c = 8 * u;
             float b[8];
             *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&sm.beta[c]);
             *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&sm.beta[c + 4]);
-            uint4 t[3], m;
-            uint32_t *th = &t[0].x, *tm = &t[1].x, *tl = &t[2].x, *mm = &m.x;
+            u64 acc[2][4] = {};
+            auto add = [&](int k, int rows_from) {   // M is zero behind the diagonal, T ahead of column c
+                float x[2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 x = *reinterpret_cast<const float2*>(&sm.A[i][c + 2 * e]);
-                split3(c + 2 * e <= i ? x.x * b[2 * e] : 0.f, c + 2 * e + 1 <= i ? x.y * b[2 * e + 1] : 0.f, th[e], tm[e], tl[e]);
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + k * 8192 + to) = t[k];
-            u64 acc[4] = {0ull, 0ull, 0ull, 0ull};
-            for (int k = c; k < 32 + 32 * (n >> 1); k += 4) {   // M is zero behind the diagonal, T ahead of column c
-                const float4 x = *reinterpret_cast<const float4*>(&M[i][k]);
-                const float xs[4] = {x.x, x.y, x.z, x.w};
+                for (int r = 0; r < 2; ++r)
+                    if (r >= rows_from) *reinterpret_cast<float4*>(x[r]) = *reinterpret_cast<const float4*>(&sm.M[lane + 32 * r][k]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const ulonglong2 y0 = *reinterpret_cast<const ulonglong2*>(&sm.A[k + j][c]), y1 = *reinterpret_cast<const ulonglong2*>(&sm.A[k + j][c + 4]);
-                    const u64 d = pk(xs[j], xs[j]);
-                    acc[0] = fma2(d, y0.x, acc[0]); acc[1] = fma2(d, y0.y, acc[1]);
-                    acc[2] = fma2(d, y1.x, acc[2]); acc[3] = fma2(d, y1.y, acc[3]);
-                }
-            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x, y;
-                unpk(acc[e], x, y);
-                mm[e] = pack_bf(x * b[2 * e], y * b[2 * e + 1]);
+                    for (int r = 0; r < 2; ++r)
+                        if (r >= rows_from) {
+                            const u64 d = pk(x[r][j], x[r][j]);
+                            acc[r][0] = fma2(d, y0.x, acc[r][0]); acc[r][1] = fma2(d, y0.y, acc[r][1]);
+                            acc[r][2] = fma2(d, y1.x, acc[r][2]); acc[r][3] = fma2(d, y1.y, acc[r][3]);
+                        }
+                }
+            };
+            for (int k = c; k < 32; k += 4) add(k, 0);
+            for (int k = max(c, 32); k < 64; k += 4) add(k, 1);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int i = lane + 32 * r;
+                const uint32_t to = (uint32_t)i * 128 + (uint32_t)((u ^ (i & 7)) * 16);
+                uint4 t[3], m;
+                uint32_t *th = &t[0].x, *tm = &t[1].x, *tl = &t[2].x, *mm = &m.x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 x = *reinterpret_cast<const float2*>(&sm.A[i][c + 2 * e]);
+                    split3(c + 2 * e <= i ? x.x * b[2 * e] : 0.f, c + 2 * e + 1 <= i ? x.y * b[2 * e + 1] : 0.f, th[e], tm[e], tl[e]);
+                    float p0, p1;
+                    unpk(acc[r][e], p0, p1);
+                    mm[e] = pack_bf(p0 * b[2 * e], p1 * b[2 * e + 1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + k * 8192 + to) = t[k];
+                *reinterpret_cast<uint4*>(to_M + to) = m;
             }
-            *reinterpret_cast<uint4*>(to_M + to) = m;
         }
         return;
     }
@@ -311,7 +335,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         for (int e = 0; e < 4; ++e) split3(v[e].x * (e < 2 ? b0.x : b1.x), v[e].y * (e < 2 ? b0.y : b1.y), s[0][e], s[1][e], s[2][e]);
 #pragma unroll
         for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + (k * kBlocks + n) * 512) = make_uint4(s[k][0], s[k][1], s[k][2], s[k][3]);
-        operand_pairs(M, mi * 16, ki * 16, lane, v);
+        operand_pairs(sm.M, mi * 16, ki * 16, lane, v);
         *reinterpret_cast<uint4*>(to_M + n * 512) =
             make_uint4(pack_bf(v[0].x, v[0].y), pack_bf(v[1].x, v[1].y), pack_bf(v[2].x, v[2].y), pack_bf(v[3].x, v[3].y));
     }

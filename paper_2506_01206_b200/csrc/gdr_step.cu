@@ -216,11 +216,18 @@ __global__ void __launch_bounds__(kThreads) gdr_sequential_kernel(const GdrPrefi
             asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         __syncthreads();
-        for (int t = 0; t < n; ++t) {
-            ulonglong2 k[KI];
+        // The output of a token is summed over its lanes together with the next token's first product, and a token's operands are fetched one token ahead.
+        ulonglong2 k[KI], q[KI];
+        float v, alpha, beta, pending = 0.f;
+        auto operands = [&](int t) {
 #pragma unroll
-            for (int i = 0; i < KI; ++i) k[i] = load4(&s.k[t][4 * j + 32 * i]);
-            const float alpha = s.alpha[t];
+            for (int i = 0; i < KI; ++i) { k[i] = load4(&s.k[t][4 * j + 32 * i]); q[i] = load4(&s.q[t][4 * j + 32 * i]); }
+            v = Act<T>::to_f32(s.v[t][row]);
+            alpha = s.alpha[t];
+            beta = s.beta[t];
+        };
+        operands(0);
+        for (int t = 0; t < n; ++t) {
             const u64 al = pk(alpha, alpha);
             u64 a = 0ull, b = 0ull;
 #pragma unroll
@@ -230,20 +237,28 @@ __global__ void __launch_bounds__(kThreads) gdr_sequential_kernel(const GdrPrefi
                 S[i].x = mul2(al, S[i].x);
                 S[i].y = mul2(al, S[i].y);
             }
-            const float nv = s.beta[t] * (Act<T>::to_f32(s.v[t][row]) - alpha * row_sum(sum2(a, b)));
+            float held = sum2(a, b);
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) {
+                held += __shfl_xor_sync(0xffffffffu, held, d);
+                pending += __shfl_xor_sync(0xffffffffu, pending, d);
+            }
+            if (j == 0 && t > 0) so[t - 1][row] = pending * p.L.scale;
+            const float nv = beta * (v - alpha * held);
             const u64 n2 = pk(nv, nv);
             u64 c = 0ull, d = 0ull;
 #pragma unroll
             for (int i = 0; i < KI; ++i) {
-                const ulonglong2 q = load4(&s.q[t][4 * j + 32 * i]);
                 S[i].x = fma2(n2, k[i].x, S[i].x);
                 S[i].y = fma2(n2, k[i].y, S[i].y);
-                c = fma2(S[i].x, q.x, c);
-                d = fma2(S[i].y, q.y, d);
+                c = fma2(S[i].x, q[i].x, c);
+                d = fma2(S[i].y, q[i].y, d);
             }
-            const float o = row_sum(sum2(c, d)) * p.L.scale;
-            if (j == 0) so[t][row] = o;
+            pending = sum2(c, d);
+            operands(min(t + 1, kTile - 1));
         }
+        pending = row_sum(pending);
+        if (j == 0) so[n - 1][row] = pending * p.L.scale;
         __syncthreads();
         if (p.L.norm_w) {
             // sum of squares of the block's rows of each token, handed to every block of the head
