@@ -300,7 +300,9 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
                         }
                 }
             };
+#pragma unroll 2
             for (int k = c; k < 32; k += 4) add(k, 0);
+#pragma unroll 2
             for (int k = max(c, 32); k < 64; k += 4) add(k, 1);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
@@ -342,26 +344,27 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
 }
 
 // ---------------------------------------------------------------- kernel 2
+constexpr int kSlice = 16, kStages = 3;
 constexpr int kChainThreads = 256;   // warps 0-3: the state's products; warps 4-7: the outputs'
 
-template <int DK, int DVS>
+template <int DK>
 struct ChainStage {
     unsigned char k[Q * DK * 2], q[Q * DK * 2];   // boxes of 64 values x 64 rows, 128-byte swizzle
     unsigned char T[kTBytes], M[kMBytes];
-    __nv_bfloat16 v[Q][DVS];
+    __nv_bfloat16 v[Q][kSlice];
     float2 csl[Q];
-    unsigned char pad[1024 - (kTBytes + kMBytes + Q * DVS * 2 + Q * 8) % 1024];
+    unsigned char pad[1024 - (kTBytes + kMBytes + Q * kSlice * 2 + Q * 8) % 1024];
 };
-template <int DK, int DVS, int STAGES>
+template <int DK>
 struct ChainSmem {
-    static constexpr int kRow = DVS + 8;                // values of a row of the operands below, padded against bank conflicts
-    ChainStage<DK, DVS> stage[STAGES];
-    float4 part[4][3][DVS / 8][32];                     // K S^T over a warp's share of d_k, for the warps of the other row tiles
-    __nv_bfloat16 S[2][DVS][DK];                        // leading part of the incoming state, by parity of the chunk; 16-byte units XOR-ed with the row index
+    static constexpr int kRow = kSlice + 8;                // values of a row of the operands below, padded against bank conflicts
+    ChainStage<DK> stage[kStages];
+    float4 part[4][3][kSlice / 8][32];                     // K S^T over a warp's share of d_k, for the warps of the other row tiles
+    __nv_bfloat16 S[2][kSlice][DK];                        // leading part of the incoming state, by parity of the chunk; 16-byte units XOR-ed with the row index
     __nv_bfloat16 R[3][Q][kRow];                        // V - e^G (K S^T), split in three
     __nv_bfloat16 W[3][Q][kRow];                        // e^{G_end - G} X, split in three
     __nv_bfloat16 X[2][2][Q][kRow];                     // X, split in two, by parity
-    uint64_t full[STAGES];
+    uint64_t full[kStages];
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
@@ -382,16 +385,16 @@ __device__ __forceinline__ void lds16(uint32_t (&r)[4], uint32_t a) {
 }
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// A state warp holds DVS x DK / 4 of the state as accumulators of the update; split in three they are, as they lie, the operands of its share of K S^T
+// A state warp holds kSlice x DK / 4 of the state as accumulators of the update; split in three they are, as they lie, the operands of its share of K S^T
 // (a quarter of d_k, all 64 tokens), so the state never passes through shared memory; the four partial sums do, to the warp of each row tile.
 // What does not depend on the product ahead is loaded before the barrier in between.  The output warps trail by half a chunk.
-template <int DK, int DVS, int STAGES>
+template <int DK>
 __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillArgs p, const GdrChunkWs ws, const __grid_constant__ GdrMaps maps, int d_v) {
-    using Smem = ChainSmem<DK, DVS, STAGES>;
+    using Smem = ChainSmem<DK>;
     constexpr int kRow = Smem::kRow;
-    constexpr int NT = DVS / 8;         // 8-column tiles of a product of 64 x DVS
+    constexpr int NT = kSlice / 8;         // 8-column tiles of a product of 64 x kSlice
     constexpr int NX = NT / 2;          // of which a state warp has these of each of two row tiles in T R
-    constexpr int MS = DVS / 16;        // 16-row tiles of the state slice
+    constexpr int MS = kSlice / 16;        // 16-row tiles of the state slice
     constexpr int ND = DK / 32;         // 8-column tiles of a warp in the state slice
     constexpr int KS = DK / 16;         // steps over d_k
     extern __shared__ __align__(1024) unsigned char s_raw[];
@@ -411,20 +414,20 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         grid_wait();
         return;
     }
-    const int khead = head / (p.L.n_v_heads / p.L.n_k_heads), col = head * d_v + slice * DVS;
+    const int khead = head / (p.L.n_v_heads / p.L.n_k_heads), col = head * d_v + slice * kSlice;
     const size_t H = p.L.n_v_heads;
     if (tid == 0) {
 #pragma unroll
-        for (int i = 0; i < STAGES; ++i) mbar_init(&sm.full[i], 1);
+        for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[i], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     grid_wait();   // T, M and the running decays are the work of the kernel just before
     __syncthreads();
     auto fetch = [&](int n) {   // one thread
-        ChainStage<DK, DVS>& s = sm.stage[n % STAGES];
-        uint64_t* bar = &sm.full[n % STAGES];
+        ChainStage<DK>& s = sm.stage[n % kStages];
+        uint64_t* bar = &sm.full[n % kStages];
         const size_t ch = (size_t)(first + n) * H + head;
-        mbar_expect_tx(bar, 2 * Q * DK * 2 + kTBytes + kMBytes + Q * DVS * 2 + Q * 8);
+        mbar_expect_tx(bar, 2 * Q * DK * 2 + kTBytes + kMBytes + Q * kSlice * 2 + Q * 8);
 #pragma unroll
         for (int h = 0; h < DK / 64; ++h) {
             tma_box(s.k + h * 8192, &maps.k, khead * DK + 64 * h, s0 + n * Q, bar);
@@ -437,11 +440,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
     };
     if (tid == kChainThreads - 32)
 #pragma unroll 1
-        for (int i = 0; i < STAGES && i < nck; ++i) fetch(i);
+        for (int i = 0; i < kStages && i < nck; ++i) fetch(i);
 
     const int g = lane >> 2, t2 = 2 * (lane & 3);
     const uint32_t sR = smem_u32(sm.R), sW = smem_u32(sm.W);
-    const int mt = warp & 3;   // row tile of the warp in products of 64 x DVS
+    const int mt = warp & 3;   // row tile of the warp in products of 64 x kSlice
     const int r0 = mt * 16 + g, r1 = r0 + 8;
     // Operand of 16 rows of keys or queries, step ks of d_k.
     auto rows_operand = [&](uint32_t (&a)[4], const unsigned char* m, int tile, int ks) {
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
     };
     bool here = true, failed = false;
     int c = 0;
-    auto arrive = [&](int n) { here = mbar_wait_bounded(&sm.full[n % STAGES], (uint32_t)(n / STAGES) & 1u) && here; };
+    auto arrive = [&](int n) { here = mbar_wait_bounded(&sm.full[n % kStages], (uint32_t)(n / kStages) & 1u) && here; };
 
     if (!outputs) {
         // State: rows (values) 16 ms + g and + 8, columns 8 (ND warp + nd) + t2 and + 1.
@@ -494,7 +497,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         const int m_of[2] = {mt < 2 ? mt : 3 - mt, mt < 2 ? 3 - mt : mt}, n_of[2] = {mt < 2 ? 0 : NX, mt < 2 ? NX : 0};
         float fr[2][2] = {{0.f, 0.f}, {0.f, 0.f}};   // decay from their rows to the chunk's end
         auto preload = [&](int n) {
-            const ChainStage<DK, DVS>& s = sm.stage[n % STAGES];
+            const ChainStage<DK>& s = sm.stage[n % kStages];
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -516,7 +519,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
             preload(0);
         }
         for (; c < nck; ++c) {
-            ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+            ChainStage<DK>& s = sm.stage[c % kStages];
             const int rows = len - c * Q;
             // K S^T over the warp's share of d_k
             float d[4][NT][4];
@@ -683,7 +686,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         }
     } else {
         for (; c < nck; ++c) {
-            const ChainStage<DK, DVS>& s = sm.stage[c % STAGES];
+            const ChainStage<DK>& s = sm.stage[c % kStages];
             const int t0 = s0 + c * Q, rows = len - c * Q;
             arrive(c);
             uint32_t qr[KS][4], mr[4][4], zr[NT][2];
@@ -705,7 +708,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
             const float e0 = ex2(s.csl[r0].x) * p.L.scale, e1 = ex2(s.csl[r1].x) * p.L.scale;
             failed = __syncthreads_or(!here);   // X and the state's leading part are there
             if (failed) break;
-            if (tid == kChainThreads - 32 && c > 0 && c - 1 + STAGES < nck) fetch(c - 1 + STAGES);   // all warps are done with the chunk before
+            if (tid == kChainThreads - 32 && c > 0 && c - 1 + kStages < nck) fetch(c - 1 + kStages);   // all warps are done with the chunk before
             // O = scale e^G (Q S^T) + M X
             float o[NT][4];
 #pragma unroll
@@ -758,7 +761,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
     }
     if (failed && tid == 0) {   // copies target this block's shared memory: one more bounded chance
         flag(p.dev_status, MDRAFT_DEV_WAIT_EXPIRED);
-        for (int i = c > 0 ? c - 1 : 0; i < (c > 0 ? c - 1 : 0) + STAGES && i < nck; ++i) mbar_wait_bounded(&sm.full[i % STAGES], (uint32_t)(i / STAGES) & 1u);
+        for (int i = c > 0 ? c - 1 : 0; i < (c > 0 ? c - 1 : 0) + kStages && i < nck; ++i) mbar_wait_bounded(&sm.full[i % kStages], (uint32_t)(i / kStages) & 1u);
     }
 }
 
@@ -811,13 +814,13 @@ inline dim3 chunk_grid(int heads, int chunks) {
     return dim3(heads, (chunks + z - 1) / z, z);
 }
 
-template <int DK, int DVS, int STAGES>
+template <int DK>
 cudaError_t chain(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps& maps, int d_v, cudaStream_t st) {
-    constexpr int smem = sizeof(ChainSmem<DK, DVS, STAGES>) + 1024;
+    constexpr int smem = sizeof(ChainSmem<DK>) + 1024;
     static_assert(smem <= 227 * 1024, "one block per SM");
-    const cudaError_t e = allow_smem<gdr_chain<DK, DVS, STAGES>>(smem);
+    const cudaError_t e = allow_smem<gdr_chain<DK>>(smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(gdr_chain<DK, DVS, STAGES>, dim3(d_v / DVS, p.L.n_v_heads, p.n_seq), kChainThreads, smem, st, p, ws, maps, d_v);
+    return launch_pdl(gdr_chain<DK>, dim3(d_v / kSlice, p.L.n_v_heads, p.n_seq), kChainThreads, smem, st, p, ws, maps, d_v);
 }
 
 template <int DK, bool kWide>
@@ -833,7 +836,7 @@ cudaError_t chunked(const GdrPrefillArgs& p, const GdrChunkWs& ws, const GdrMaps
     cudaError_t e = slice == d_v ? prepare<DK, true>(p, ws, maps, st) : prepare<DK, false>(p, ws, maps, st);
     if (e != cudaSuccess) return e;
     if (slice == d_v) return launch_gdr_chain_wide(p, ws, maps, DK, d_v, st);
-    e = slice == 16 ? chain<DK, 16, 3>(p, ws, maps, d_v, st) : chain<DK, 32, 2>(p, ws, maps, d_v, st);
+    e = chain<DK>(p, ws, maps, d_v, st);
     if (e != cudaSuccess || !ws.o) return e;
     return launch_pdl(d_v == 128 ? gdr_norm_gate<128> : gdr_norm_gate<64>, chunk_grid(p.L.n_v_heads, p.n_chunks_bound), kNormThreads, 0, st, p, ws.o);
 }

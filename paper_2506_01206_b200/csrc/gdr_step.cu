@@ -217,17 +217,22 @@ __global__ void __launch_bounds__(kThreads) gdr_sequential_kernel(const GdrPrefi
         }
         __syncthreads();
         // The output of a token is summed over its lanes together with the next token's first product, and a token's operands are fetched one token ahead.
-        ulonglong2 k[KI], q[KI];
-        float v, alpha, beta, pending = 0.f;
-        auto operands = [&](int t) {
+        ulonglong2 k[KI], q[KI], k_next[KI], q_next[KI];
+        float v, alpha, beta, v_next, alpha_next, beta_next, pending = 0.f;
+        auto fetch_next = [&](int t) {
 #pragma unroll
-            for (int i = 0; i < KI; ++i) { k[i] = load4(&s.k[t][4 * j + 32 * i]); q[i] = load4(&s.q[t][4 * j + 32 * i]); }
-            v = Act<T>::to_f32(s.v[t][row]);
-            alpha = s.alpha[t];
-            beta = s.beta[t];
+            for (int i = 0; i < KI; ++i) { k_next[i] = load4(&s.k[t][4 * j + 32 * i]); q_next[i] = load4(&s.q[t][4 * j + 32 * i]); }
+            v_next = Act<T>::to_f32(s.v[t][row]);
+            alpha_next = s.alpha[t];
+            beta_next = s.beta[t];
         };
-        operands(0);
+        fetch_next(0);
+#pragma unroll 2
         for (int t = 0; t < n; ++t) {
+#pragma unroll
+            for (int i = 0; i < KI; ++i) { k[i] = k_next[i]; q[i] = q_next[i]; }
+            v = v_next; alpha = alpha_next; beta = beta_next;
+            fetch_next(min(t + 1, n - 1));
             const u64 al = pk(alpha, alpha);
             u64 a = 0ull, b = 0ull;
 #pragma unroll
@@ -255,7 +260,6 @@ __global__ void __launch_bounds__(kThreads) gdr_sequential_kernel(const GdrPrefi
                 d = fma2(S[i].y, q[i].y, d);
             }
             pending = sum2(c, d);
-            operands(min(t + 1, kTile - 1));
         }
         pending = row_sum(pending);
         if (j == 0) so[n - 1][row] = pending * p.L.scale;
