@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                     }
                 }
             }
-            if (p.io.z) arrive(&sm.z_free);
+            if (p.io.z && ok) arrive(&sm.z_free);   // not after a wait that ran out: the barrier of a copy that is still expected must not be armed again
         }
     } else if (warp == kMmaWarp) {
         // ---------------------------------------------------------------- products
