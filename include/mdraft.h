@@ -442,7 +442,8 @@ int mdraft_ssd_tree_step(const mdraft_ssd_layer *layer, const mdraft_cache *cach
  * The bracketed parts are left out where norm_w / z is NULL.  q, k and v are taken as given: a block convolves its q | k | v
  * channels with a MDRAFT_CONV_ONLY call over a layer of that many channels (the same state pool holds the windows) and brings
  * the query and key heads to unit length with mdraft_qk_norm.  Keys have to keep beta * |k|^2 at 2 or less, as unit keys do: with larger ones the
- * recurrence itself grows without bound.
+ * recurrence itself grows without bound.  A NaN or infinity among a token's q, k, v, dt or beta stays with its sequence, and there reaches, as in the
+ * recurrence, the tokens behind it; a long sequence is encoded 64 tokens at a time, and then it may reach tokens of the same 64 ahead of it as well.
  *
  * Supported: d_k and d_v 64 or 128, n_v_heads a multiple of n_k_heads, fp32 or bf16 activations; anything else is
  * MDRAFT_ERR_UNSUPPORTED.  State slots: (n_v_heads * d_v, d_k) fp32 in an mdraft_cache, whose windows these calls do not touch (cache->conv may
@@ -468,8 +469,9 @@ typedef struct {
  *   are neither read into a result nor written
  *   max_seqlen: an upper bound on the longest sequence (HOST value): with its help the call chooses how it works; the results do not
  *               depend on it beyond rounding
- *   workspace : device scratch of at least mdraft_gdr_prefill_workspace_bytes(...) bytes, 256-byte aligned; NULL where that is 0.  `out` must not
- *               overlap an input
+ *   workspace : device scratch of at least mdraft_gdr_prefill_workspace_bytes(...) bytes, 256-byte aligned; NULL where that is 0.  Its contents
+ *               need not be initialised; calls that may run at the same time (other streams, graphs replayed side by side) each need their own.
+ *               `out` must not overlap an input, and no two sequences may end in one slot
  */
 size_t mdraft_gdr_prefill_workspace_bytes(const mdraft_gdr_layer *layer, int32_t total_tokens, int32_t n_seq, int32_t max_seqlen);
 
@@ -510,7 +512,7 @@ int mdraft_gdr_tree_step(const mdraft_gdr_layer *layer, const mdraft_cache *cach
  *              q_out may be q with the same stride, k_out likewise (in place); no other overlap.  One of the head counts may be 0
  *   positions: (rows) int32, may be NULL when rot_dim is 0
  * Supported: d_head a multiple of 8 up to 256; rot_dim even and at most d_head, a multiple of 16 for MDRAFT_ROT_HALF; fp32 or bf16
- * activations; anything else is MDRAFT_ERR_UNSUPPORTED.  No counterpart in the paper, which does not look inside a layer.
+ * activations, n_rows up to 2^31 - 4097; anything else is MDRAFT_ERR_UNSUPPORTED.  No counterpart in the paper, which does not look inside a layer.
  */
 enum { MDRAFT_NORM_NONE = 0, MDRAFT_NORM_L2 = 1, MDRAFT_NORM_RMS = 2 };
 enum { MDRAFT_ROT_HALF = 0, MDRAFT_ROT_PAIRS = 1 };

@@ -1203,6 +1203,7 @@ int mdraft_qk_norm(const mdraft_qk_norm_spec* spec, const void* q, int64_t ldq, 
     if (spec->rot_dim > d || spec->rot_dim % (spec->rot_layout == MDRAFT_ROT_HALF ? 16 : 2) != 0) return MDRAFT_ERR_UNSUPPORTED;
     if (spec->rot_dim > 0 && !spec->freqs) return MDRAFT_ERR_INVALID_ARG;
     if ((spec->q_w && !aligned16(spec->q_w)) || (spec->k_w && !aligned16(spec->k_w))) return MDRAFT_ERR_MISALIGNED;
+    if (n_rows > kQkNormMaxRows) return MDRAFT_ERR_UNSUPPORTED;
     if (n_rows == 0 || spec->n_q_heads + spec->n_k_heads == 0) return MDRAFT_OK;
     int rc;
     if ((rc = check_matrix(q, ldq, spec->n_q_heads * d, act, spec->n_q_heads > 0))) return rc;

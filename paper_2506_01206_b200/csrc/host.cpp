@@ -563,12 +563,29 @@ float attr_float(PyObject* owner, PyObject* name) {
     return (float)v;
 }
 
-void on_current_device(const at::Tensor& t, const char* name) {
-    if (!t.is_cuda() || t.get_device() != c10::cuda::current_device()) fail(PyExc_ValueError, std::string(name) + ": must be a CUDA tensor of the current device");
-}
+// The current device, asked for once per call.
+struct Device {
+    int index = -1;
+    void holds(const at::Tensor& t, const char* name) {
+        if (t.is_cuda()) {
+            if (index < 0) index = c10::cuda::current_device();
+            if (t.get_device() == index) return;
+        }
+        fail(PyExc_ValueError, std::string(name) + ": must be a CUDA tensor of the current device");
+    }
+    // Constants of a layer or a spec, whose types and sizes its constructor has looked at; None = absent.
+    const float* constants(PyObject* owner, PyObject* name) {
+        Ref r(PyObject_GetAttr(owner, name));
+        if (r.p == Py_None) return nullptr;
+        const char* text = PyUnicode_AsUTF8(name);
+        const at::Tensor& t = tensor(r.p, text);
+        holds(t, text);
+        return static_cast<const float*>(t.const_data_ptr());
+    }
+};
 
 // Rows of `cols` activations; None = absent, where that is allowed.  `rows` < 0: any number.
-Matrix activations(PyObject* o, const char* name, int act, int64_t cols, int64_t rows, bool optional = false) {
+Matrix activations(Device& dev, PyObject* o, const char* name, int act, int64_t cols, int64_t rows, bool optional = false) {
     if (o == Py_None && !optional) fail(PyExc_TypeError, std::string(name) + ": must be a tensor");
     Matrix m(Py_None, name);
     if (o == Py_None) return m;
@@ -576,7 +593,8 @@ Matrix activations(PyObject* o, const char* name, int act, int64_t cols, int64_t
     if (t.dim() == 2 && t.size(0) == 0) { m.p = t.const_data_ptr(); m.ld = cols; }   // strides of nothing mean nothing
     else m = Matrix(o, name);
     if (m.rows == 1) m.ld = cols;   // nor does the step to a second row that is not there
-    on_current_device(t, name);
+    dev.holds(t, name);
+    if (t.size(0) > INT32_MAX) fail(PyExc_ValueError, std::string(name) + ": too many rows");
     if (t.scalar_type() != (act == MDRAFT_BF16 ? at::kBFloat16 : at::kFloat)) fail(PyExc_TypeError, std::string(name) + ": must have the layer's activation dtype");
     if (t.size(1) != cols || (rows >= 0 && t.size(0) != rows))
         fail(PyExc_ValueError, std::string(name) + ": need " + (rows >= 0 ? std::to_string(rows) + " x " : std::string("rows of ")) + std::to_string(cols) + " values");
@@ -584,40 +602,39 @@ Matrix activations(PyObject* o, const char* name, int act, int64_t cols, int64_t
 }
 
 // Contiguous int32 indices of the current device; None = absent.
-const int32_t* device_indices(PyObject* o, int64_t n, const char* name) {
+const int32_t* device_indices(Device& dev, PyObject* o, int64_t n, const char* name) {
     if (o == Py_None) return nullptr;
     const at::Tensor& t = tensor(o, name);
     if (t.scalar_type() != at::kInt) fail(PyExc_TypeError, std::string(name) + " must be int32");
-    on_current_device(t, name);
+    dev.holds(t, name);
     if ((n >= 0 && t.numel() != n) || !t.is_contiguous()) fail(PyExc_ValueError, std::string(name) + ": need " + std::to_string(n) + " contiguous entries");
     return static_cast<const int32_t*>(t.const_data_ptr());
 }
 
-int32_t* status_word(PyObject* o) {
+int32_t* status_word(Device& dev, PyObject* o) {
     if (o != Py_None && (tensor(o, "dev_status").scalar_type() != at::kInt || tensor(o, "dev_status").numel() < 1)) fail(PyExc_TypeError, "dev_status must be int32");
-    if (o != Py_None) on_current_device(tensor(o, "dev_status"), "dev_status");
+    if (o != Py_None) dev.holds(tensor(o, "dev_status"), "dev_status");
     return static_cast<int32_t*>(mutable_data(o, "dev_status"));
 }
 
-mdraft_gdr_layer gdr_layer_of(PyObject* o, PyObject* flags) {
+mdraft_gdr_layer gdr_layer_of(Device& dev, PyObject* o, PyObject* flags) {
     mdraft_gdr_layer l;
     l.n_k_heads = (int32_t)attr_int(o, N.n_k_heads); l.n_v_heads = (int32_t)attr_int(o, N.n_v_heads);
     l.d_k = (int32_t)attr_int(o, N.d_k); l.d_v = (int32_t)attr_int(o, N.d_v);
     l.act = act_of(o);
     l.flags = (uint32_t)(flags == Py_None ? attr_int(o, N.flags) : as_int(flags));
     l.scale = attr_float(o, N.scale); l.eps = attr_float(o, N.eps);
-    l.A = static_cast<const float*>(attr_data(o, N.A)); l.dt_bias = static_cast<const float*>(attr_data(o, N.dt_bias));
-    l.norm_w = static_cast<const float*>(attr_data(o, N.norm_w));
+    l.A = dev.constants(o, N.A); l.dt_bias = dev.constants(o, N.dt_bias); l.norm_w = dev.constants(o, N.norm_w);
     return l;
 }
 
 // A pool of delta-layer states: fp32, as wide as the layer, dense slots, on the current device.
 struct States : Cache {
-    States(PyObject* o, const mdraft_gdr_layer& l) : Cache(o) {
+    States(Device& dev, PyObject* o, const mdraft_gdr_layer& l) : Cache(o) {
         if (!present) return;
         Ref s(PyObject_GetAttr(o, N.ssm));
         const at::Tensor& t = tensor(s.p, "ssm");
-        on_current_device(t, "the cache");
+        dev.holds(t, "the cache");
         if (t.scalar_type() != at::kFloat || t.dim() != 4 || t.size(2) != (int64_t)l.n_v_heads * l.d_v || t.size(3) != l.d_k || t.stride(3) != 1 || t.stride(2) != l.d_k)
             fail(PyExc_ValueError, "the cache's slots must be fp32 states of n_v_heads * d_v rows of d_k values");
     }
@@ -627,26 +644,30 @@ struct States : Cache {
 struct GdrTensors {
     Matrix v, q, k, z, dt, beta, out;
     int64_t rows;
-    GdrTensors(PyObject* const* a, const mdraft_gdr_layer& l)
-        : v(activations(a[2], "v", l.act, (int64_t)l.n_v_heads * l.d_v, -1)),
-          q(activations(a[0], "q", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)), k(activations(a[1], "k", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)),
-          z(activations(a[3], "z", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows, true)), dt(activations(a[4], "dt", l.act, l.n_v_heads, v.rows)),
-          beta(activations(a[5], "beta", l.act, l.n_v_heads, v.rows)), out(activations(a[6], "out", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows)), rows(v.rows) {}
+    GdrTensors(Device& dev, PyObject* const* a, const mdraft_gdr_layer& l)
+        : v(activations(dev, a[2], "v", l.act, (int64_t)l.n_v_heads * l.d_v, -1)),
+          q(activations(dev, a[0], "q", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)), k(activations(dev, a[1], "k", l.act, (int64_t)l.n_k_heads * l.d_k, v.rows)),
+          z(activations(dev, a[3], "z", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows, true)), dt(activations(dev, a[4], "dt", l.act, l.n_v_heads, v.rows)),
+          beta(activations(dev, a[5], "beta", l.act, l.n_v_heads, v.rows)), out(activations(dev, a[6], "out", l.act, (int64_t)l.n_v_heads * l.d_v, v.rows)), rows(v.rows) {}
 };
 
 // (table, layer, cache, layer_index, q, k, v, z, dt, beta, out, cu_seqlens, max_seqlen, init_slot, final_slot, workspace, dev_status,
 //  stream, flags)
 PyObject* gdr_prefill(PyObject* const* a) {
-    const mdraft_gdr_layer l = gdr_layer_of(a[1], a[18]);
-    const States c(a[2], l);
+    Device dev;
+    const mdraft_gdr_layer l = gdr_layer_of(dev, a[1], a[18]);
+    const States c(dev, a[2], l);
     const int32_t li = (int32_t)as_int(a[3]), longest = (int32_t)as_int(a[12]);
-    const GdrTensors t(a + 4, l);
-    const int32_t* cu = device_indices(a[11], -1, "cu_seqlens");
+    const GdrTensors t(dev, a + 4, l);
+    const int32_t* cu = device_indices(dev, a[11], -1, "cu_seqlens");
     const int64_t n_seq = cu ? tensor(a[11], "cu_seqlens").numel() - 1 : 1;
-    const int32_t *init = device_indices(a[13], n_seq, "init_slot"), *fin = device_indices(a[14], n_seq, "final_slot");
+    const int32_t *init = device_indices(dev, a[13], n_seq, "init_slot"), *fin = device_indices(dev, a[14], n_seq, "final_slot");
     const Workspace ws(a[15]);
-    if (ws.p) on_current_device(tensor(a[15], "workspace"), "workspace");
-    int32_t* st = status_word(a[16]);
+    if (ws.p) {
+        dev.holds(tensor(a[15], "workspace"), "workspace");
+        if (!tensor(a[15], "workspace").is_contiguous()) fail(PyExc_ValueError, "workspace: must be contiguous");
+    }
+    int32_t* st = status_word(dev, a[16]);
     void* stream = stream_of(a[17]);
     const Entry& e = entry(a[0]);
     return released([&] {
@@ -657,13 +678,14 @@ PyObject* gdr_prefill(PyObject* const* a) {
 
 // (table, layer, cache, layer_index, q, k, v, z, dt, beta, out, parent_slot, node_slot, level_offsets, dev_status, stream, flags)
 PyObject* gdr_tree_step(PyObject* const* a) {
-    const mdraft_gdr_layer l = gdr_layer_of(a[1], a[16]);
-    const States c(a[2], l);
+    Device dev;
+    const mdraft_gdr_layer l = gdr_layer_of(dev, a[1], a[16]);
+    const States c(dev, a[2], l);
     const int32_t li = (int32_t)as_int(a[3]);
-    const GdrTensors t(a + 4, l);
-    const int32_t *parent = device_indices(a[11], t.rows, "parent_slot"), *node = device_indices(a[12], t.rows, "node_slot");
+    const GdrTensors t(dev, a + 4, l);
+    const int32_t *parent = device_indices(dev, a[11], t.rows, "parent_slot"), *node = device_indices(dev, a[12], t.rows, "node_slot");
     const Levels lv(a[13]);
-    int32_t* st = status_word(a[14]);
+    int32_t* st = status_word(dev, a[14]);
     void* stream = stream_of(a[15]);
     const Entry& e = entry(a[0]);
     return released([&] {
@@ -674,14 +696,19 @@ PyObject* gdr_tree_step(PyObject* const* a) {
 
 // (table, cache, src_slot, dst_slot, dev_status, stream)
 PyObject* gdr_commit(PyObject* const* a) {
+    Device dev;
     const Cache c(a[1]);
     if (!c.present) fail(PyExc_TypeError, "cache must not be None");
+    {
+        Ref s(PyObject_GetAttr(a[1], N.ssm));
+        dev.holds(tensor(s.p, "ssm"), "the cache");
+    }
     const int32_t d = (int32_t)attr_int(a[1], N.d_inner), n = (int32_t)attr_int(a[1], N.d_state), w = (int32_t)attr_int(a[1], N.d_conv);
     const int32_t channels = (int32_t)attr_int(a[1], N.conv_channels);
     const int act = act_of(a[1]);
     const int64_t m = tensor(a[2], "src_slot").numel();
-    const int32_t *src = device_indices(a[2], m, "src_slot"), *dst = device_indices(a[3], m, "dst_slot");
-    int32_t* st = status_word(a[4]);
+    const int32_t *src = device_indices(dev, a[2], m, "src_slot"), *dst = device_indices(dev, a[3], m, "dst_slot");
+    int32_t* st = status_word(dev, a[4]);
     void* stream = stream_of(a[5]);
     const Entry& e = entry(a[0]);
     return released([&] { return e.gdr_commit(c.get(), d, n, channels, w, act, (int32_t)m, src, dst, st, stream); });
@@ -689,20 +716,20 @@ PyObject* gdr_commit(PyObject* const* a) {
 
 // (table, spec, q, k, q_out, k_out, positions, stream)
 PyObject* qk_norm(PyObject* const* a) {
+    Device dev;
     mdraft_qk_norm_spec s;
     PyObject* o = a[1];
     s.d_head = (int32_t)attr_int(o, N.d_head); s.n_q_heads = (int32_t)attr_int(o, N.n_q_heads); s.n_k_heads = (int32_t)attr_int(o, N.n_k_heads);
     s.act = act_of(o);
     s.norm = (int32_t)attr_int(o, N.norm); s.rot_dim = (int32_t)attr_int(o, N.rot_dim); s.rot_layout = (int32_t)attr_int(o, N.rot_layout);
     s.eps = attr_float(o, N.eps); s.rot_scale = attr_float(o, N.rot_scale);
-    s.q_w = static_cast<const float*>(attr_data(o, N.q_w)); s.k_w = static_cast<const float*>(attr_data(o, N.k_w));
-    s.freqs = static_cast<const float*>(attr_data(o, N.freqs));
+    s.q_w = dev.constants(o, N.q_w); s.k_w = dev.constants(o, N.k_w); s.freqs = dev.constants(o, N.freqs);
     const int64_t qc = (int64_t)s.n_q_heads * s.d_head, kc = (int64_t)s.n_k_heads * s.d_head;
     const bool no_q = s.n_q_heads == 0, no_k = s.n_k_heads == 0;
-    const Matrix q(activations(a[2], "q", s.act, qc, -1, no_q)), k(activations(a[3], "k", s.act, kc, no_q ? -1 : q.rows, no_k));
+    const Matrix q(activations(dev, a[2], "q", s.act, qc, -1, no_q)), k(activations(dev, a[3], "k", s.act, kc, no_q ? -1 : q.rows, no_k));
     const int64_t rows = no_q ? k.rows : q.rows;
-    const Matrix qo(activations(a[4], "q_out", s.act, qc, rows, no_q)), ko(activations(a[5], "k_out", s.act, kc, rows, no_k));
-    const int32_t* pos = device_indices(a[6], rows, "positions");
+    const Matrix qo(activations(dev, a[4], "q_out", s.act, qc, rows, no_q)), ko(activations(dev, a[5], "k_out", s.act, kc, rows, no_k));
+    const int32_t* pos = device_indices(dev, a[6], rows, "positions");
     void* stream = stream_of(a[7]);
     const Entry& e = entry(a[0]);
     return released([&] { return e.qk_norm(&s, q.p, q.ld, k.p, k.ld, qo.out(), qo.ld, ko.out(), ko.ld, pos, (int32_t)rows, stream); });

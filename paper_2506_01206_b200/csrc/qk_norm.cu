@@ -18,6 +18,8 @@ namespace {
 template <typename T> constexpr int kItemsOf = 8 / sizeof(T);   // heads a lane group has in flight: 64 bytes a lane
 constexpr int kThreads = 256, kMaxThreads = 512;       // of a block as a rule, and where the heads of a row ask for more
 
+constexpr size_t kMaxTurnBytes = 48 * 1024;             // of shared memory, what a block may have without asking
+
 // Two times four values as they lie in memory.
 template <typename T> struct Raw;
 template <> struct Raw<float> {
@@ -169,10 +171,12 @@ cudaError_t launch(const QkNormArgs& p, cudaStream_t st) {
     auto passes = [&] { return (p.rows + cut.row_lanes * cut.items - 1) / (cut.row_lanes * cut.items); };
     while (cut.items > 1 && passes() * (int64_t)parts < 2 * sm_count()) --cut.items;
     while (cut.row_lanes > 1 && passes() * (int64_t)parts < 2 * sm_count()) cut.row_lanes /= 2;
+    auto smem_bytes = [&] { return 2 * (size_t)(cut.row_lanes * cut.items) * ((p.rot_dim / 2 + 3) & ~3) * sizeof(float2); };
+    while (cut.items > 1 && smem_bytes() > kMaxTurnBytes) --cut.items;   // one or two heads to a row, most of their values turned
     cut.passes = passes();
     const int most = (2 * kMaxThreads / threads) * sm_count() / parts;   // resident at once
     const int blocks = cut.passes < most ? cut.passes : (most > 0 ? most : 1);
-    const size_t smem = 2 * (size_t)(cut.row_lanes * cut.items) * ((p.rot_dim / 2 + 3) & ~3) * sizeof(float2);
+    const size_t smem = smem_bytes();
     if (p.rot_layout == MDRAFT_ROT_HALF) qk_norm_kernel<T, G, true><<<dim3(blocks, parts), threads, smem, st>>>(p, cut);
     else qk_norm_kernel<T, G, false><<<dim3(blocks, parts), threads, smem, st>>>(p, cut);
     return cudaGetLastError();

@@ -5,6 +5,8 @@
 
 namespace mdraft {
 
+constexpr int kQkNormMaxRows = 0x7fffffff - 4096;   // the last pass may count this far past the end
+
 struct QkNormArgs {
     const void *q, *k;
     void *q_out, *k_out;

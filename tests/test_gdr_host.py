@@ -150,3 +150,8 @@ def test_the_extension_checks_how_many_arguments_it_is_given(lib, name, count):
     for n in (0, count - 1, count + 1):
         with pytest.raises(TypeError, match=f"expected {count} arguments, got {n}"):
             f(*[None] * n)
+
+
+def test_more_rows_than_the_norm_counts_are_refused(lib):
+    s = _spec(rot_dim=0)
+    assert _norm(lib, s, n=2 ** 31 - 1) == UNSUPPORTED and _norm(lib, s, n=2 ** 31 - 4096) == UNSUPPORTED
