@@ -14,15 +14,18 @@
 // chain over the chunks of a sequence, kernel 2, whose rows of S (values) are independent: a block takes a slice of them.
 //
 //   1. gdr_chunk_prepare, a block per (value head, chunk): [K; Q] K^T as one product of 128 rows on the tensor cores (tcgen05, operands by
-//      TMA), then the triangle's inverse by forward substitution in fp32, a column per thread.  Results go to the workspace in
-//      the order in which kernel 2's lanes hold them.
-//   2. gdr_chain, a block per (slice of d_v, value head, sequence): state in registers, three small products per chunk one after another
-//      (K S^T; T times the difference; the update), beside them the two of the outputs.
-//   3. gdr_norm_gate where there is an output norm, which needs all slices of a row.
+//      TMA), then the triangle's inverse in fp32: its diagonal blocks of 16 by forward substitution, a column per lane, the blocks below by two rounds of
+//      products (of the 16s, of the 32s).  Results go to the workspace in the order in which kernel 2's lanes hold them.  Bound by shared-memory
+//      latency: 2048 tokens x 12 heads 13 us, 141000 x 12 0.65 ms (for the wide chain, with M T).
+//   2. gdr_chain, a block per (slice of 16 values, value head, sequence): state in registers, three small products per chunk one after another
+//      (K S^T; T times the difference; the update), beside them the two of the outputs.  2048 tokens: 64 us, 2 us a chunk whatever the width up to the SMs' number
+//      of blocks.  Where there are many chains a block takes a whole head instead (gdr_wide.cu).
+//   3. gdr_norm_gate where there is an output norm, which needs all slices of a row (the wide chain does it itself).  10 us for 2048 tokens x 12 heads.
 //
 // Precision.  States keep fp32 accuracy: q, k, v are bf16 as given; everything else that meets them in a product of the state's path (S, T, the
 // differences, X) is split into three bf16 values (24 bits), which costs three products with an exact operand and six where both are
-// split.  Two values (16 bits) left an error of 3e-6 in the states.  The outputs' products take S and M as one bf16 value and X as two.
+// split.  Two values (16 bits) left an error of 3e-6 in the states.  The outputs' products take S and M as one bf16 value and X as two: what they lose is the size
+// of the outputs' own rounding.  Running log decays are summed in 64 bits and kept as two fp32 values, as differences of sums of 10^4 are wanted to 2^-24.
 //
 // Kernel 2 runs on the warp-level tensor instructions (mma.sync), not on tcgen05: its products are 64 x 16 x 128 and depend on
 // one another, so what counts is the way from one to the next (registers to shared memory and back, a barrier) and not the rate.
