@@ -8,7 +8,7 @@
 // either half in a lane (two loads of 8 or 16 bytes), so that it takes none.  The turns of a row (position times frequency, reduced
 // to [-1/2, 1/2] turns in 64 bits, as an fp32 product is off by whole radians at positions of a million) are formed once and shared by its heads
 // through shared memory.  A block works through passes of rows and has the next one's loads in flight meanwhile.  Bound: memory.  Measured (bf16, 12 + 4 heads): heads of 64, 32
-// values turned, 141000 rows 120 us, 4.8 TB/s (200 us with one head per thread and pass, without loads ahead); heads of 128, all turned, 2048 rows 8.2 us.
+// values turned, 141000 rows 112 us, 5.2 TB/s (200 us with one head per thread and pass, without loads ahead; issue slots are nearly as full); heads of 128, all turned, 2048 rows 8.2 us.
 #include "common.cuh"
 #include "qk_norm.cuh"
 
@@ -21,38 +21,45 @@ constexpr int kThreads = 256, kMaxThreads = 512;       // of a block as a rule, 
 
 constexpr size_t kMaxTurnBytes = 48 * 1024;             // of shared memory, what a block may have without asking
 
-// Two times four values as they lie in memory.
+// Two times four values as they lie in memory, beside one another or not, and as packed pairs of fp32.
 template <typename T> struct Raw;
 template <> struct Raw<float> {
     float4 a, b;
+    template <bool kBeside>
     __device__ __forceinline__ void load(const float* p, int to_b) {
         a = *reinterpret_cast<const float4*>(p);
-        b = *reinterpret_cast<const float4*>(p + to_b);
+        b = *reinterpret_cast<const float4*>(p + (kBeside ? 4 : to_b));
     }
-    __device__ __forceinline__ void widen(float (&v)[8]) const { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w; }
+    __device__ __forceinline__ void widen(u64 (&v)[4]) const { v[0] = pk(a.x, a.y); v[1] = pk(a.z, a.w); v[2] = pk(b.x, b.y); v[3] = pk(b.z, b.w); }
+    template <bool kBeside>
     __device__ static __forceinline__ void store(float* p, int to_b, const float (&v)[8]) {
         *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(p + to_b) = make_float4(v[4], v[5], v[6], v[7]);
+        *reinterpret_cast<float4*>(p + (kBeside ? 4 : to_b)) = make_float4(v[4], v[5], v[6], v[7]);
     }
 };
 template <> struct Raw<__nv_bfloat16> {
-    uint2 a, b;
+    uint4 w;
+    template <bool kBeside>
     __device__ __forceinline__ void load(const __nv_bfloat16* p, int to_b) {
-        a = *reinterpret_cast<const uint2*>(p);
-        b = *reinterpret_cast<const uint2*>(p + to_b);
+        if (kBeside) { w = *reinterpret_cast<const uint4*>(p); return; }
+        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + to_b);
+        w = make_uint4(a.x, a.y, b.x, b.y);
     }
-    __device__ __forceinline__ void widen(float (&v)[8]) const {
-        const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+    __device__ __forceinline__ void widen(u64 (&v)[4]) const {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        for (int i = 0; i < 4; ++i) v[i] = pk(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
     }
     __device__ static __forceinline__ uint32_t pack(float lo, float hi) {
         const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&b);
     }
+    template <bool kBeside>
     __device__ static __forceinline__ void store(__nv_bfloat16* p, int to_b, const float (&v)[8]) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack(v[0], v[1]), pack(v[2], v[3]));
-        *reinterpret_cast<uint2*>(p + to_b) = make_uint2(pack(v[4], v[5]), pack(v[6], v[7]));
+        const uint2 a = make_uint2(pack(v[0], v[1]), pack(v[2], v[3])), b = make_uint2(pack(v[4], v[5]), pack(v[6], v[7]));
+        if (kBeside) { *reinterpret_cast<uint4*>(p) = make_uint4(a.x, a.y, b.x, b.y); return; }
+        *reinterpret_cast<uint2*>(p) = a;
+        *reinterpret_cast<uint2*>(p + to_b) = b;
     }
 };
 
@@ -80,29 +87,36 @@ __global__ void __launch_bounds__(kMaxThreads, 2) qk_norm_kernel(const QkNormArg
     if (h >= p.n_q_heads + p.n_k_heads) from = static_cast<const T*>(p.n_q_heads ? p.q : p.k);
     const int reach = mine ? to_b : 4;
     const float per_value = p.norm == MDRAFT_NORM_RMS ? 1.0f / (float)p.d_head : 1.0f;
-    float weight[8];
+    u64 weight[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) weight[e] = 1.0f;
+    for (int e = 0; e < 4; ++e) weight[e] = pk(1.0f, 1.0f);
     if (const float* w = key ? p.k_w : p.q_w; w && mine && p.norm != MDRAFT_NORM_NONE)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) weight[e] = __ldg(w + at + (e < 4 ? e : to_b + e - 4));
+        for (int e = 0; e < 4; ++e) {
+            const float* pair = w + at + (e < 2 ? 2 * e : to_b + 2 * e - 4);
+            weight[e] = pk(__ldg(pair), __ldg(pair + 1));
+        }
     Raw<T> raw[kItems];
     auto load = [&](int pass) {
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int row = pass * per_pass + i * cut.row_lanes + lane_row;
-            if (i < cut.items) raw[i].load(from + (row < p.rows ? row : p.rows - 1) * ld, reach);
+            if (i < cut.items) raw[i].template load<!kHalf>(from + (row < p.rows ? row : p.rows - 1) * ld, reach);
         }
     };
+    const int step_r = half > 0 ? blockDim.x / half : 0, step_c = half > 0 ? blockDim.x - step_r * half : 0;   // of the next value a thread turns
     auto turn = [&](int pass, float2* out) {
         const int row0 = pass * per_pass, n = min(per_pass, p.rows - row0) * half;
+        int r = tid / half, c = tid - r * half;
         for (int i = tid; i < n; i += blockDim.x) {
-            const int r = i / half, c = i - r * half;
             double t = (double)__ldg(p.positions + row0 + r) * (double)__ldg(p.freqs + c) * 0.15915494309189535;   // in turns
             t -= rint(t);
             float sn, cs;
             sincospif((float)(2.0 * t), &sn, &cs);
             out[r * pitch + c] = make_float2(cs * p.rot_scale, sn * p.rot_scale);
+            r += step_r;
+            c += step_c;
+            if (c >= half) { c -= half; ++r; }
         }
     };
     const int pairs = kHalf ? 4 : (p.rot_dim - 8 * l) / 2;   // of the lane that are turned
@@ -123,19 +137,24 @@ __global__ void __launch_bounds__(kMaxThreads, 2) qk_norm_kernel(const QkNormArg
         for (int i = 0; i < kItems; ++i) {   // lanes without a head take part in the shuffles
             if (i >= cut.items) break;
             const int row = pass * per_pass + i * cut.row_lanes + lane_row;
-            float x[8];
-            now[i].widen(x);
+            u64 v[4];
+            now[i].widen(v);
             if (p.norm != MDRAFT_NORM_NONE) {
-                float sq = 0.f;
+                u64 sum = 0ull;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
-                if (!mine) sq = 0.f;
+                for (int e = 0; e < 4; ++e) sum = fma2(v[e], v[e], sum);
+                float sq, odd;
+                unpk(sum, sq, odd);
+                sq = mine ? sq + odd : 0.f;
 #pragma unroll
                 for (int o = 1; o < G; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
                 const float f = rsqrtf(fmaf(sq, per_value, p.eps));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= f * weight[e];
+                for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], mul2(pk(f, f), weight[e]));
             }
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) unpk(v[e], x[2 * e], x[2 * e + 1]);
             if (turned) {
                 const float4* t = reinterpret_cast<const float4*>(tr + i * cut.row_lanes * pitch + 4 * l);
                 const float4 t0 = t[0], t1 = t[1];
@@ -151,7 +170,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) qk_norm_kernel(const QkNormArg
                     }
                 }
             }
-            if (mine && row < p.rows) Raw<T>::store(to + row * ldo, to_b, x);
+            if (mine && row < p.rows) Raw<T>::template store<!kHalf>(to + row * ldo, to_b, x);
         }
         if (half > 0 && next < cut.passes) {
             turn(next, turns + (buffer ^ 1) * per_pass * pitch);
