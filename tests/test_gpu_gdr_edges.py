@@ -195,3 +195,21 @@ def test_norm_rows_whose_offsets_pass_32_bits():
     md.mdraft_qk_norm(spec, big[:, -384:-128], big[:, -128:], big[:, -384:-128], big[:, -128:], pos)
     torch.cuda.synchronize()
     assert same(o, big[:, -384:])
+
+
+@pytest.mark.parametrize("hv", [2, 40])
+def test_a_nan_reaches_nothing_ahead_of_its_64_tokens(hv):
+    """What the encode says of a NaN among a sequence's own values: it stays with the sequence and behind the start of its 64 tokens."""
+    p = Problem(400, 2, hv, seed=70)
+    cu, final = i32([0, 200, 400]), i32([0, 1])
+    res = []
+    for poison in (False, True):
+        if poison:
+            p.dev[2][100].fill_(float("nan"))
+        out, cache = p.out(), p.cache(2)
+        md.mdraft_gdr_prefill(p.layer, cache, 0, *p.dev, out, cu, 200, None, final, p.workspace(2, 200))
+        torch.cuda.synchronize()
+        res.append((out, cache.ssm[0].clone()))
+    (a, sa), (b, sb) = res
+    assert same(a[:64], b[:64]) and same(a[200:], b[200:]) and torch.equal(sa[1], sb[1])
+    assert bool(b[100:200].isnan().all()) and bool(sb[0].isnan().any())
