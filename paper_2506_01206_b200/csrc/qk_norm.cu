@@ -77,14 +77,14 @@ __global__ void __launch_bounds__(kMaxThreads, 2) qk_norm_kernel(const QkNormArg
     const int tid = threadIdx.x, l = tid % G, group = tid / G;
     const int lane_row = group / cut.heads, in_part = group - lane_row * cut.heads, half = p.rot_dim / 2, pitch = (half + 3) & ~3;
     const int h = blockIdx.y * cut.heads + in_part, per_pass = cut.row_lanes * cut.items;
-    const bool key = h >= p.n_q_heads, mine = lane_row < cut.row_lanes && h < p.n_q_heads + p.n_k_heads && 8 * l < p.d_head;
+    const bool key = h >= p.n_q_heads && p.n_k_heads > 0;   // (a group behind the last head reads along with its rows and strides, and writes nothing)
+    const bool mine = lane_row < cut.row_lanes && h < p.n_q_heads + p.n_k_heads && 8 * l < p.d_head;
     // A rotation by halves takes four values of either half into a lane, so that every pair is in one lane.
     const bool turned = 8 * l < p.rot_dim;
     const int at = kHalf && turned ? 4 * l : 8 * l, to_b = kHalf && turned ? half : 4;
     const int64_t column = mine ? (int64_t)(key ? h - p.n_q_heads : h) * p.d_head + at : 0, ld = key ? p.ldk : p.ldq, ldo = key ? p.ldko : p.ldqo;
-    const T* from = static_cast<const T*>(key ? p.k : p.q) + column;   // lanes without a share of a head read something, and write nothing
+    const T* from = static_cast<const T*>(key ? p.k : p.q) + column;
     T* to = static_cast<T*>(key ? p.k_out : p.q_out) + column;
-    if (h >= p.n_q_heads + p.n_k_heads) from = static_cast<const T*>(p.n_q_heads ? p.q : p.k);
     const int reach = mine ? to_b : 4;
     const float per_value = p.norm == MDRAFT_NORM_RMS ? 1.0f / (float)p.d_head : 1.0f;
     u64 weight[4];

@@ -213,3 +213,24 @@ def test_a_nan_reaches_nothing_ahead_of_its_64_tokens(hv):
     (a, sa), (b, sb) = res
     assert same(a[:64], b[:64]) and same(a[200:], b[200:]) and torch.equal(sa[1], sb[1])
     assert bool(b[100:200].isnan().all()) and bool(sb[0].isnan().any())
+
+
+@pytest.mark.parametrize("hq,hk,apart", [(40, 1, "k"), (1, 40, "q"), (33, 0, "q"), (0, 33, "k")])
+def test_norm_of_queries_and_keys_with_strides_far_apart(hq, hk, apart):
+    """More heads than a block takes, so that its last groups have none: they keep to one operand's rows and strides (read with the other's, the rows of the
+    narrow one would end long before)."""
+    rows, d = 5, 128
+    wide = lambda x: torch.zeros((rows, 1 << 20), dtype=torch.bfloat16, device="cuda").index_copy_(1, torch.arange(x.shape[1], device="cuda"), x)[:, :x.shape[1]]
+    q, k = (torch.randn((rows, h * d), device="cuda").bfloat16() if h else None for h in (hq, hk))
+    spec = md.QkNorm(d, hq, hk)
+    new = lambda x: None if x is None else torch.empty_like(x)
+    want = [new(q), new(k)]
+    md.mdraft_qk_norm(spec, q, k, *want)
+    far = [wide(q) if apart == "q" else q, wide(k) if apart == "k" else k]
+    got = [new(q), new(k)]
+    md.mdraft_qk_norm(spec, *far, *got)
+    torch.cuda.synchronize()
+    for a, b, x, h in zip(want, got, (q, k), (hq, hk)):
+        if h:
+            assert torch.equal(a, b)
+            check(a, gdr.head_norm(x.double().cpu().numpy(), d, "l2"), d, 0, "half", "bf16")
