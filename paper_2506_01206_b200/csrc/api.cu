@@ -1038,10 +1038,10 @@ struct GdrPlan {
     size_t off_M, off_csl, off_o, bytes;
 };
 
-// The longest sequence that is done token by token.  A token takes 0.13 to 0.18 us there, the shortest call in chunks 14 us; with more heads and sequences both grow, token
-// by token earlier.  Measured (bf16, 128 x 128, token by token against chunks): 12 heads 33 tokens 9.0 against 13.6 us, 64 12.7 against 14.9, 96 17.1 against 16.9; four
-// sequences of 33 tokens 14.5 against 21.6, 64 22.5 against 22.1, 80 27.0 against 26.4; eight (more than gdr_few_rows) 24 tokens 17.2 against 22.8, 33 22.7
-// against 23.3, 48 28.9 against 23.4.  The least favourable: four sequences of 64 tokens x 4 heads, 16.7 against 15.0.
+// The longest sequence that is done token by token.  A token takes 0.12 to 0.16 us there, the shortest call in chunks 14 us; with more heads and sequences both grow, token
+// by token earlier.  Measured (bf16, 128 x 128, token by token against chunks): 12 heads 33 tokens 8.7 against 13.6 us, 64 11.9 against 14.9, 96 16.0 against 16.8; four
+// sequences of 33 tokens 14.7 against 21.6, 64 21.7 against 22.1, 96 30.0 against 27.3; eight (more than gdr_few_rows) 24 tokens 17.2 against 23.0, 33 22.8
+// against 23.5, 48 28.7 against 23.6.  The least favourable: four sequences of 64 tokens x 4 heads, 16.0 against 15.0.
 int gdr_sequential_max(const mdraft_gdr_layer* L, int n_seq) { return gdr_few_rows(L->n_v_heads, L->d_v, n_seq) ? 64 : 32; }
 
 GdrPlan plan_gdr(const mdraft_gdr_layer* L, int T, int n_seq, int max_seqlen) {

@@ -36,9 +36,9 @@ struct GdrPrefillArgs {
 };
 
 // Token by token: one kernel, no workspace.  Blocks hold 16 rows of a state where the call has few of them, else 32: 16 rows are one warp to a scheduler, whose tokens take
-// 0.13 us instead of 0.18, but the same work is more blocks and more copies of a head's keys.  Measured (16 against 32 rows; 128 x 128): 12 heads x 32 tokens 8.1
-// against 10.0 us, fp32 512 tokens 78 against 114, four such 163 against 204; eight sequences of 32 tokens (5.2 blocks of 16 to an SM) 23.5 against 21.0, eight of 512
-// in fp32 333 against 312.
+// 0.12 us instead of 0.16, but the same work is more blocks and more copies of a head's keys.  Measured (16 against 32 rows; 128 x 128): 12 heads x 32 tokens 7.7
+// against 9.7 us, fp32 512 tokens 72 against 108, four such 159 against 201; six sequences of 512 in fp32 (3.9 blocks of 16 to an SM) 307 against 305. Beyond, 16 rows lose: eight
+// sequences of 32 tokens (5.2 blocks to an SM) 23.5 against 21.0, eight of 512 in fp32 333 against 312.
 inline bool gdr_few_rows(int n_v_heads, int d_v, int n_seq) { return (int64_t)n_v_heads * (d_v / 16) * n_seq <= 4 * sm_count(); }
 cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int act, cudaStream_t st);
 

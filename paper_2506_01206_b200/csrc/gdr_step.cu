@@ -16,9 +16,9 @@
 //
 // The token-by-token encode keeps the state in registers for the whole sequence; 16 or 32 rows to a block, so that a head of 128 rows is
 // a cluster of eight or four blocks, which exchange their sums of squares for the output norm through distributed shared memory.  It is
-// bound by the latency of one token's chain (dot product, three shuffles, update): 0.13 us a token where a scheduler has one warp of rows.  So the warps that hold
+// bound by the latency of one token's chain (dot product, three shuffles, update): 0.11 to 0.14 us a token where a scheduler has one warp of rows.  So the warps that hold
 // the state do nothing else; four helper warps bring the tiles of 16 tokens, and sum, norm, gate and store a tile's outputs while the next is at work
-// (fp32, 12 heads of 128 x 128, 512 tokens: 164 us where all warps did both, 78 with the helpers and 16 rows).  Taking the product with the next key ahead of the
+// (fp32, 12 heads of 128 x 128, 512 tokens: 164 us where all warps did both, 72 with the helpers and 16 rows).  Taking the product with the next key ahead of the
 // update (by the recurrence of the products, through k_{t-1} . k_t) shortens the chain on paper and won nothing: what it saves it adds in instructions.
 #include "chunk_map.cuh"
 #include "common.cuh"
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(8 * R + kHelpers, kSeqBlocks<T, DK, R>) gdr_se
                 beta_next = s.beta[t];
             };
             fetch_next(0);
-#pragma unroll 2
+#pragma unroll 8   // (against 2: 56.8 -> 51.2 us for 480 tokens of 64 values)
             for (int t = 0; t < n; ++t) {
 #pragma unroll
                 for (int i = 0; i < KI; ++i) { k[i] = widen(k_next[i]); q[i] = widen(q_next[i]); }
