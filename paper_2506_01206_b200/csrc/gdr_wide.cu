@@ -10,7 +10,7 @@
 //
 // S itself stays in registers (fp32), the operands of the other side (K, Q, T, M T) come by TMA as they are used.  M T instead of M makes the outputs
 // wait for R, not for X.  Three products of a chunk depend on one another; in between 256 threads take accumulators to operands: tensor
-// memory -> registers -> tensor memory.  A chunk of 128 x 128 costs some 9000 cycles, of which the products are 2300; the rest is the way between them, where the
+// memory -> registers -> tensor memory.  A chunk of 128 x 128 costs 9000 cycles, 11000 with all SMs at work, of which the products are 2300; the rest is the way between them, where the
 // splitting into three parts alone takes 16 cycles of a scheduler per pair of values and warp.  With as many chains as SMs or more that beats the narrow chain, whose
 // blocks share a head among eight SMs to be done with a chunk in 3900 (measured where the choice is made).  32 sequences of 1000 to 8000 tokens x 12 heads: 1.18 ms for
 // the chain and 0.65 ms for the triangles ahead of it, 1.9 ms in all against 10.7 token by token.
