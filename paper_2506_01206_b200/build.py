@@ -12,6 +12,8 @@ turns a call's tensors into the library's arguments.  ``build_library(variant="w
 ``libmdraft_waittest.so``, for the failure-path tests: the same sources with a
 short limit on every on-chip wait and an overstated byte count on every
 copy barrier, so that each bounded wait runs out and the give-up paths execute.
+``build_library(variant="holdtest")`` builds a third, ``libmdraft_holdtest.so``, for the ordering tests: warps are held up
+where a late warp must do no harm.
 """
 
 from __future__ import annotations
@@ -36,6 +38,7 @@ NVCC_FLAGS = [
 # name -> (library file, extra compile flags)
 VARIANTS = {
     "": (LIB, []),
+    "holdtest": (os.path.join(HERE, "libmdraft_holdtest.so"), ["-DMDRAFT_TEST_HOLD_UP_NS=50000u"]),
     "waittest": (os.path.join(HERE, "libmdraft_waittest.so"), ["-DMDRAFT_SPIN_LIMIT=4096u", "-DMDRAFT_TEST_OVERSTATE_TX=16u"]),
 }
 
@@ -119,5 +122,5 @@ def build_host(force: bool = False) -> str:
 
 
 if __name__ == "__main__":
-    variant = "waittest" if "--waittest" in sys.argv else ""
+    variant = next((v for v in VARIANTS if v and f"--{v}" in sys.argv), "")
     print(build_library(force=True, verbose="-v" in sys.argv, variant=variant))

@@ -31,6 +31,15 @@ constexpr uint32_t kSpinLimit = MDRAFT_SPIN_LIMIT;
 constexpr uint32_t kOverstateTx = MDRAFT_TEST_OVERSTATE_TX;
 constexpr uint32_t kPollNs = 1000u;
 
+// Third build of the library, for the ordering tests only: a warp is held up for this long where its being late has to be harmless, so that
+// an order that only timing provides shows in the results.
+#ifndef MDRAFT_TEST_HOLD_UP_NS
+#define MDRAFT_TEST_HOLD_UP_NS 0u
+#endif
+__device__ __forceinline__ void test_hold_up() {
+    if constexpr (MDRAFT_TEST_HOLD_UP_NS > 0u) __nanosleep(MDRAFT_TEST_HOLD_UP_NS);
+}
+
 // ---------------------------------------------------------------- scalar math
 __device__ __forceinline__ float ex2(float v) {
     float r;

@@ -48,7 +48,7 @@ struct WideSmem {
     __nv_bfloat16 z[Q][DV];      // gate
     float eo[Q];                 // decay from the chunk's start times scale, for the output warps (which may fall behind the stages)
     float o[Q][DV + 4];          // outputs on their way from a lane per value to a row per warp
-    uint64_t full[kStages], done[kStages];                   // copies of a stage, all products that read it
+    uint64_t full[kStages], done[kStages];                   // copies of a stage, all products that read it (and, through w, all that the state warps read of it)
     uint64_t state[2], r[2], w[2], free_o;                   // operands are in tensor memory (in two portions), output accumulators have been read
     uint64_t mma1, mma2, out, last;                          // products
     uint64_t z_full, z_free;
@@ -250,6 +250,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
             wait(&sm.mma2, c);
             tc_fence_after();
             load_d1();
+            const float all = s.ef[Q - 1].x;
 #pragma unroll
             for (int hand = 0; hand < 2; ++hand) {
                 u64 x[4];
@@ -260,7 +261,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                 }
                 hand_over(x, kW[0], kW[1], kW[2], hand, &sm.w[hand]);
             }
-            const float all = s.ef[Q - 1].x;
+            // From here on no state warp touches the stage: the arrivals on w[1] are all that `done` waits for, and behind `done` chunk c + 2 is copied into it.
+            if (warp == 5) test_hold_up();
             wait(&sm.done[c % kStages], c / kStages);
             tc_fence_after();
             if (rows_here && ok) {
