@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int head = blockIdx.x, cidx = blockIdx.y + blockIdx.z * gridDim.y;
     grid_wait();
-    grid_release_dependents();
+    if (!kWide) grid_release_dependents();
     const ChunkInfo ci = find_chunk(p.cu, p.n_seq, p.T, Q, p.n_chunks_bound, cidx);
     if (ci.seq < 0) return;
     const int rows = ci.t1 - ci.t0;
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
             tma_box(sm.kq + h * 16384 + 8192, &maps.q, kcol + 64 * h, ci.t0, &sm.bar_tma);
         }
     }
-    if (warp == 3) { tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
+    if (warp == 3) { test_hold_up(); tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
     float g = 0.f, beta = 0.f;   // rows past the chunk's end: no decay, nothing written
     if (tid < rows) {
         const size_t t = (size_t)(ci.t0 + tid);
@@ -147,6 +147,9 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     }
     if (tid == 31) sm.warp_sum = sum;
     __syncthreads();
+    // The wide chain takes all of an SM's tensor memory and then waits for this kernel's end: its blocks may start only once every block here has its own columns, or
+    // one that shares an SM with them would wait for theirs for good.
+    if (kWide) grid_release_dependents();
     tc_fence_after();
     if (tid < Q) {
         if (warp == 1) sum += sm.warp_sum;

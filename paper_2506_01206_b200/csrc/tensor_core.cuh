@@ -33,6 +33,8 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 }
 
 // Tensor memory: allocation (one warp), release, and the accumulator loads (a warp reads the 32 lanes it owns).
+// An allocation waits, without a limit, until the columns are free.  So a kernel whose dependent allocates ahead of its own grid_wait releases dependents only
+// behind its own allocation, unless the blocks that fit an SM together never want more than its 512 columns (the SSD encode: three of at most 128).
 __device__ __forceinline__ void tmem_alloc(uint32_t* slot_in_smem, uint32_t cols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot_in_smem)), "r"(cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");

@@ -43,3 +43,16 @@ def test_a_late_warp_of_the_chain_reads_its_own_chunk(heldlib, hk, hv, dk, dv):
     with using(heldlib):
         got = encode(p, [500])
     assert torch.equal(got[1], want[1]) and torch.equal(got[0].view(torch.int16), want[0].view(torch.int16))
+
+
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 64, 64), (1, 1, 128, 64), (1, 1, 128, 128)])
+def test_a_block_late_with_its_tensor_memory_is_not_shut_out(heldlib, hk, hv, dk, dv):
+    """Many short sequences, so that blocks of the chain are ready long before the last chunk's block of the kernel ahead has looked up what it works on: they
+    do not start, and take the SMs' tensor memory, before that one has its own."""
+    lens = list(np.random.default_rng(3).integers(1, 71, 1500))
+    p = Problem(int(sum(lens)), hk, hv, dk, dv, seed=81)
+    assert is_chunked(p, lens)
+    want = encode(p, lens)
+    with using(heldlib):
+        got = encode(p, lens)
+    assert torch.equal(got[1], want[1]) and torch.equal(got[0].view(torch.int16), want[0].view(torch.int16))
