@@ -53,6 +53,7 @@ struct WideSmem {
     uint64_t mma1, mma2, out, last;                          // products
     uint64_t z_full, z_free;
     uint32_t tmem_base;
+    int picked;                                              // the block's sequence (a word that no copy targets: copies are not ordered behind ordinary accesses)
 };
 
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -91,7 +92,6 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
     grid_release_dependents();
     int seq = blockIdx.y;
     if (p.n_seq > 1 && p.n_seq <= kMaxSorted) {   // the longest sequences first: the blocks that start last are to be the short ones
-        int* const pick = reinterpret_cast<int*>(&sm);
         if (tid < p.n_seq) {
             int a, mine, b, other;
             bool bad_a, bad_b;
@@ -101,11 +101,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                 seq_span(p.cu, p.n_seq, p.T, i, b, other, bad_b);
                 rank += other > mine || (other == mine && i < tid);
             }
-            if (rank == (int)blockIdx.y) *pick = tid;
+            if (rank == (int)blockIdx.y) sm.picked = tid;
         }
         __syncthreads();
-        seq = *pick;
-        __syncthreads();
+        seq = sm.picked;
     }
     int first, nck, s0, len;
     bool bad;

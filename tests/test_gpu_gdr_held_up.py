@@ -56,3 +56,17 @@ def test_a_block_late_with_its_tensor_memory_is_not_shut_out(heldlib, hk, hv, dk
     with using(heldlib):
         got = encode(p, lens)
     assert torch.equal(got[1], want[1]) and torch.equal(got[0].view(torch.int16), want[0].view(torch.int16))
+
+
+@pytest.mark.parametrize("n", [2, 19, 512])
+def test_sequences_taken_by_length_keep_their_rows_and_slots(n):
+    """Lengths in an order unlike their ranks, equal ones among them: every sequence equals the same sequence in a call that does not rank (one of 600)."""
+    lens = [int(v) for v in np.random.default_rng(n).choice([1, 40, 64, 70, 129, 130], n)]
+    lens[0], lens[-1] = 40, 130
+    hv = 152 // n + 1 if n < 38 else 2
+    p = Problem(sum(lens), 1, hv, 64, 128, seed=82)
+    assert is_chunked(p, lens)
+    want = encode(p, lens)
+    more = lens + [0] * (600 - n)
+    got = encode(p, more)
+    assert torch.equal(got[1][:, :n], want[1]) and torch.equal(got[0].view(torch.int16), want[0].view(torch.int16))
