@@ -401,7 +401,8 @@ def mdraft_tree_step_proj(layer: Layer, cache: StateCache, layer_index: int, W_x
 
 def mdraft_state_commit(cache: StateCache, src_slot: torch.Tensor, dst_slot: torch.Tensor,
                         dev_status: Optional[torch.Tensor] = None, stream=None) -> None:
-    if cache is not None and (cache.conv_channels != cache.d_inner or cache.d_state == 64):   # slots of a delta layer
+    channels = getattr(cache, "conv_channels", None)   # a pool of the caller's own need not say how wide its windows are
+    if channels is not None and (channels != cache.d_inner or cache.d_state == 64):   # slots of a delta layer
         mdraft_gdr_state_commit(cache, src_slot, dst_slot, dev_status, stream)
         return
     rc = _host.commit(_entry(), cache, src_slot, dst_slot, dev_status, stream)

@@ -155,3 +155,21 @@ def test_the_extension_checks_how_many_arguments_it_is_given(lib, name, count):
 def test_more_rows_than_the_norm_counts_are_refused(lib):
     s = _spec(rot_dim=0)
     assert _norm(lib, s, n=2 ** 31 - 1) == UNSUPPORTED and _norm(lib, s, n=2 ** 31 - 4096) == UNSUPPORTED
+
+
+def test_a_commit_takes_any_cache_that_has_a_pools_attributes(monkeypatch):
+    """mdraft_state_commit reads the attributes of a pool and no more: one without `conv_channels` has windows as wide as its states, and goes the ordinary way."""
+    import types
+
+    import paper_2506_01206_b200 as md
+    from paper_2506_01206_b200 import binding
+    calls = []
+    fake = types.SimpleNamespace(commit=lambda *a: calls.append("ordinary") or 0, gdr_commit=lambda *a: calls.append("delta") or 0)
+    monkeypatch.setattr(binding, "_host", fake)
+    monkeypatch.setattr(binding, "_entry", lambda: None)
+    pool = lambda **kw: types.SimpleNamespace(**{**dict(d_inner=512, d_state=16, d_conv=4, act=torch.bfloat16, n_layers=1, n_slots=4), **kw})
+    for cache, way in ((pool(), "ordinary"), (pool(d_state=128), "ordinary"), (pool(d_state=64), "ordinary"), (pool(conv_channels=512), "ordinary"),
+                       (pool(d_state=128, conv_channels=1024), "delta"), (pool(d_state=64, conv_channels=512), "delta"), (None, "ordinary")):
+        calls.clear()
+        md.mdraft_state_commit(cache, None, None)
+        assert calls == [way]
