@@ -48,7 +48,7 @@ constexpr uint32_t kGdrWideTBytes = 24576, kGdrWideMBytes = 8192;   // the wide 
 struct GdrChunkWs {
     unsigned char* T;   // (1 + A)^-1 diag(beta), split into three bf16 values
     unsigned char* M;   // masked products of queries and keys, bf16; for the wide chain times T
-    float2* csl;        // 64 running log2 decays (value, remainder); for the wide chain decays from the chunk's start and to its end
+    float2* ef;         // decays of 64 rows: from the chunk's start, to its end
     float* o;           // (T, Hv * d_v) fp32 outputs before the norm; NULL: there is no norm, or the chain does it
 };
 
@@ -75,16 +75,37 @@ struct GdrStepArgs {
 cudaError_t launch_gdr_step(const GdrStepArgs& p, int d_k, int d_v, int act, cudaStream_t st);
 
 // ---------------------------------------------------------------- device helpers shared by the kernels
-// Decay and write strength of one token and head: alpha = exp(Delta A), beta (MDRAFT_BETA_SIGMOID: of its pre-activation).
-template <typename T>
-__device__ __forceinline__ float gdr_log2_decay(const GdrLayerDev& L, const T* dt, int head) {
-    const float v = Act<T>::to_f32(*dt) + (L.dt_bias ? __ldg(L.dt_bias + head) : 0.f);
-    return ((L.flags & MDRAFT_DT_SOFTPLUS) ? softplus(v) : v) * __ldg(L.A + head) * kLog2e;
+// 2^(hi + lo) to about one unit of the last place (the hardware's 2^x is off by up to four): a decay is multiplied into the state token after token or chunk after
+// chunk, so what it is off by adds up over as many as a head remembers.  hi = n + f, and e^y, y = (f + lo) ln 2, by its Taylor series (|y| <= 0.347: what follows y^7 / 7! is
+// below 6e-9).  2^n comes in two factors, as n may go past the exponent's range either way.
+__device__ __forceinline__ float exp2_f32(float hi, float lo) {
+    hi = hi < -252.f ? -252.f : (hi > 252.f ? 252.f : hi);   // (a NaN stays one)
+    const float n = rintf(hi), y = ((hi - n) + lo) * kLn2;
+    float e = fmaf(y, 1.0f / 5040, 1.0f / 720);
+    e = fmaf(y, e, 1.0f / 120);
+    e = fmaf(y, e, 1.0f / 24);
+    e = fmaf(y, e, 1.0f / 6);
+    e = fmaf(y, e, 0.5f);
+    e = fmaf(y * y, e, y) + 1.0f;
+    const int half = (int)n >> 1, rest = (int)n - half;
+    return e * __int_as_float((half + 127) << 23) * __int_as_float((rest + 127) << 23);
 }
+__device__ __forceinline__ float exp_f32(float x) {
+    x = x < -174.f ? -174.f : (x > 174.f ? 174.f : x);
+    const float hi = x * kLog2e;
+    return exp2_f32(hi, fmaf(x, 1.92596299e-8f, fmaf(x, kLog2e, -hi)));   // log2 e = kLog2e + 1.926e-8
+}
+// Step size of a token and head times A: the log of its decay.
+template <typename T>
+__device__ __forceinline__ float gdr_log_decay(const GdrLayerDev& L, const T* dt, int head) {
+    const float v = Act<T>::to_f32(*dt) + (L.dt_bias ? __ldg(L.dt_bias + head) : 0.f);
+    return ((L.flags & MDRAFT_DT_SOFTPLUS) ? (v > 20.f ? v : log1pf(exp_f32(v))) : v) * __ldg(L.A + head);
+}
+// Write strength beta (MDRAFT_BETA_SIGMOID: of its pre-activation).
 template <typename T>
 __device__ __forceinline__ float gdr_beta(const GdrLayerDev& L, const T* b) {
     const float v = Act<T>::to_f32(*b);
-    return (L.flags & MDRAFT_BETA_SIGMOID) ? rcp(1.0f + ex2(-kLog2e * v)) : v;
+    return (L.flags & MDRAFT_BETA_SIGMOID) ? __frcp_rn(1.0f + exp_f32(-v)) : v;
 }
 
 }  // namespace mdraft

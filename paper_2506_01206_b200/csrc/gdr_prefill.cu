@@ -132,14 +132,14 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         }
     }
     if (warp == 3) { test_hold_up(); tmem_alloc(&sm.tmem_base, 64); tc_fence_before(); }
-    float g = 0.f, beta = 0.f;   // rows past the chunk's end: no decay, nothing written
+    float beta = 0.f;   // rows past the chunk's end: no decay, nothing written
+    double sum = 0.0;
     if (tid < rows) {
         const size_t t = (size_t)(ci.t0 + tid);
-        g = gdr_log2_decay(p.L, static_cast<const __nv_bfloat16*>(p.io.dt) + t * p.io.lddt + head, head);
+        sum = 1.4426950408889634 * gdr_log_decay(p.L, static_cast<const __nv_bfloat16*>(p.io.dt) + t * p.io.lddt + head, head);
         beta = gdr_beta(p.L, static_cast<const __nv_bfloat16*>(p.io.beta) + t * p.io.ldb + head);
     }
     // Running sums in 64 bits, kept as two fp32 values: what is wanted is their differences, and a head that forgets at once sums to 10^4.
-    double sum = g;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const double up = __shfl_up_sync(0xffffffffu, sum, o);
@@ -156,10 +156,9 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
         const float hi = (float)sum;
         sm.csl[tid] = make_float2(hi, (float)(sum - hi));
         sm.beta[tid] = beta;
-        if (!kWide) ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = sm.csl[tid];
     }
     __syncthreads();
-    if (kWide && tid < Q) ws.csl[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = make_float2(ex2(sm.csl[tid].x), ex2(log2_between(sm.csl[tid], sm.csl[Q - 1])));
+    if (tid < Q) ws.ef[((size_t)cidx * p.L.n_v_heads + head) * Q + tid] = make_float2(exp2_f32(sm.csl[tid].x, sm.csl[tid].y), exp2_f32(log2_between(sm.csl[tid], sm.csl[Q - 1]), 0.f));
     const uint32_t tmem = sm.tmem_base;
     const bool in_ok = mbar_wait_bounded(&sm.bar_tma, 0u);
     if (in_ok && tid == 0) {
@@ -358,7 +357,7 @@ struct ChainStage {
     unsigned char k[Q * DK * 2], q[Q * DK * 2];   // boxes of 64 values x 64 rows, 128-byte swizzle
     unsigned char T[kTBytes], M[kMBytes];
     __nv_bfloat16 v[Q][kSlice];
-    float2 csl[Q];
+    float2 ef[Q];   // decay from the chunk's start to a row, from the row to the chunk's end
     unsigned char pad[1024 - (kTBytes + kMBytes + Q * kSlice * 2 + Q * 8) % 1024];
 };
 template <int DK>
@@ -442,7 +441,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         tma_box(s.v, &maps.v, col, s0 + n * Q, bar);
         bulk_load(s.T, ws.T + ch * kTBytes, kTBytes, bar);
         bulk_load(s.M, ws.M + ch * kMBytes, kMBytes, bar);
-        bulk_load(s.csl, ws.csl + ch * Q, Q * 8, bar);
+        bulk_load(s.ef, ws.ef + ch * Q, Q * 8, bar);
     };
     if (tid == kChainThreads - 32)
 #pragma unroll 1
@@ -513,12 +512,11 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 vr[i][0] = *reinterpret_cast<const uint32_t*>(&s.v[r0][i * 8 + t2]);
                 vr[i][1] = *reinterpret_cast<const uint32_t*>(&s.v[r1][i * 8 + t2]);
             }
-            const float2 end = s.csl[Q - 1], c0 = s.csl[r0], c1 = s.csl[r1];
-            e0 = ex2(c0.x); e1 = ex2(c1.x); ec = ex2(end.x);
+            e0 = s.ef[r0].x; e1 = s.ef[r1].x; ec = s.ef[Q - 1].x;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) fr[i][h] = ex2(log2_between(s.csl[m_of[i] * 16 + g + 8 * h], end));
+                for (int h = 0; h < 2; ++h) fr[i][h] = s.ef[m_of[i] * 16 + g + 8 * h].y;
         };
         if (nck > 0) {
             arrive(0);
@@ -711,7 +709,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                     if (r1 < rows) zr[n][1] = *reinterpret_cast<const uint32_t*>(z + 8 * p.io.ldz + n * 8 + t2);
                 }
             }
-            const float e0 = ex2(s.csl[r0].x) * p.L.scale, e1 = ex2(s.csl[r1].x) * p.L.scale;
+            const float e0 = s.ef[r0].x * p.L.scale, e1 = s.ef[r1].x * p.L.scale;
             failed = __syncthreads_or(!here);   // X and the state's leading part are there
             if (failed) break;
             if (tid == kChainThreads - 32 && c > 0 && c - 1 + kStages < nck) fetch(c - 1 + kStages);   // all warps are done with the chunk before

@@ -78,8 +78,7 @@ __global__ void __launch_bounds__(kThreads, 2) gdr_step_kernel(const GdrStepArgs
     for (int i = 0; i < KI; ++i) { k[i] = load4(kr + 32 * i); q[i] = load4(qr + 32 * i); }
 #pragma unroll
     for (int r = 0; r < NP; ++r) v[r] = Act<T>::to_f32(vr[row0 + r * kRowsPerPass]);
-    const float alpha = ex2(gdr_log2_decay(p.L, static_cast<const T*>(p.io.dt) + (size_t)node * p.io.lddt + head, head));
-    const float beta = gdr_beta(p.L, static_cast<const T*>(p.io.beta) + (size_t)node * p.io.ldb + head);
+    const T dt_raw = static_cast<const T*>(p.io.dt)[(size_t)node * p.io.lddt + head], beta_raw = static_cast<const T*>(p.io.beta)[(size_t)node * p.io.ldb + head];
     float z = 0.f, w = 1.f;
     if (tid < DV) {
         if (p.io.z) z = Act<T>::to_f32(static_cast<const T*>(p.io.z)[(size_t)node * p.io.ldz + (size_t)head * DV + tid]);
@@ -98,6 +97,7 @@ __global__ void __launch_bounds__(kThreads, 2) gdr_step_kernel(const GdrStepArgs
             S[r][i] = make_ulonglong2(0ull, 0ull);
             if (pslot >= 0) S[r][i] = *reinterpret_cast<const ulonglong2*>(hp + (size_t)r * kRowsPerPass * DK + 32 * i);
         }
+    const float alpha = exp_f32(gdr_log_decay(p.L, &dt_raw, head)), beta = gdr_beta(p.L, &beta_raw);   // while the state is on its way
     const u64 al = pk(alpha, alpha);
     float o[NP], sq = 0.f;
 #pragma unroll
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(8 * R + kHelpers, kSeqBlocks<T, DK, R>) gdr_se
     };
     auto put_gates = [&](int tile) {
         if (h < kTile) {
-            sm.tile[tile % kStages].alpha[h] = ex2(gdr_log2_decay(p.L, &dt_raw, head));
+            sm.tile[tile % kStages].alpha[h] = exp_f32(gdr_log_decay(p.L, &dt_raw, head));
             sm.tile[tile % kStages].beta[h] = gdr_beta(p.L, &beta_raw);
         }
     };

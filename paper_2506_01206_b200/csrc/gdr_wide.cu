@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
         const size_t col = (size_t)head * DV + lane * E;
         for (int c = 0; c < nck; ++c) {
             const int t0 = s0 + c * Q, rows = min(Q, len - c * Q);
-            if (w < 2) sm.eo[row] = p.L.scale * ws.csl[((size_t)(first + c) * H + head) * Q + row].x;
+            if (w < 2) sm.eo[row] = p.L.scale * ws.ef[((size_t)(first + c) * H + head) * Q + row].x;
             bar_sync(kBarRows, 128);   // and the rows' staging is free
             wait(&sm.out, c);
             tc_fence_after();
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                 tma_box(s.v, &maps.v, head * DV, s0 + c * Q, bar);
                 bulk_load(s.T, ws.T + ch * kGdrWideTBytes, kGdrWideTBytes, bar);
                 bulk_load(s.M, ws.M + ch * kGdrWideMBytes, kGdrWideMBytes, bar);
-                bulk_load(s.ef, ws.csl + ch * Q, Q * 8, bar);
+                bulk_load(s.ef, ws.ef + ch * Q, Q * 8, bar);
             }
             __syncwarp();
         }
