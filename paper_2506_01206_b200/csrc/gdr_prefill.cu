@@ -137,6 +137,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     if (tid < rows) {
         const size_t t = (size_t)(ci.t0 + tid);
         sum = 1.4426950408889634 * gdr_log_decay(p.L, static_cast<const __nv_bfloat16*>(p.io.dt) + t * p.io.lddt + head, head);
+        if (sum < -256.0) sum = -256.0;   // no fp32 value survives that, and the running sums behind a step of 10^12 keep their last bits
         beta = gdr_beta(p.L, static_cast<const __nv_bfloat16*>(p.io.beta) + t * p.io.ldb + head);
     }
     // Running sums in 64 bits, kept as two fp32 values: what is wanted is their differences, and a head that forgets at once sums to 10^4.

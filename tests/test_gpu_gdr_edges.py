@@ -234,3 +234,22 @@ def test_norm_of_queries_and_keys_with_strides_far_apart(hq, hk, apart):
         if h:
             assert torch.equal(a, b)
             check(a, gdr.head_norm(x.double().cpu().numpy(), d, "l2"), d, 0, "half", "bf16")
+
+
+@pytest.mark.parametrize("huge", [1e4, 1e12, 3e38, float("inf")])
+@pytest.mark.parametrize("n,hv", [(24, 2), (200, 2), (200, 40)])
+def test_one_token_that_forgets_everything_leaves_the_decays_behind_it_exact(n, hv, huge):
+    """A step size that takes the decay to zero, however large: what the tokens behind it write decays as ever."""
+    p = Problem(n, 1, hv, seed=71)
+    p.np["dt"][[5, n // 2, n // 2 + 1, n - 10]] = torch.tensor(huge).bfloat16().float().item()
+    p.upload()
+    cache, out, status = p.cache(2), p.out(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    h0 = p.states(1)
+    cache.ssm[0, 0] = torch.from_numpy(h0[0]).cuda()
+    md.mdraft_gdr_prefill(p.layer, cache, 0, *p.dev, out, None, n, i32([0]), i32([1]), p.workspace(1, n), status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    with np.errstate(over="ignore"):
+        w_out, w_states, o, size, size64 = gdr.encode(**p.args(), cu=[0, n], S0=h0, sizes=True)
+    check_states(cache.ssm[0, 1], np.asarray(w_states)[0])
+    p.check_out(out, w_out, o, size, size64 if is_chunked(p, [n]) else None)
