@@ -40,8 +40,8 @@ namespace {
 
 constexpr int Q = kGdrQ;
 constexpr int kBlocks = 10;                            // 16 x 16 blocks of a lower triangle of 64 x 64
-constexpr uint32_t kTBytes = kGdrTBytes, kMBytes = kGdrMBytes;
-static_assert(kTBytes == 3 * kBlocks * 512 && kMBytes == kBlocks * 512, "workspace layout");
+constexpr uint32_t kTBytes = kGdrTBytes, kMBytes = kGdrMBytes, kMPart = kBlocks * 512;
+static_assert(kTBytes == 3 * kMPart && kMBytes == 2 * kMPart, "workspace layout");
 
 // ---------------------------------------------------------------- kernel 1
 constexpr int kPrepThreads = 128;
@@ -79,7 +79,11 @@ __device__ __forceinline__ void operand_pairs(const float (*m)[kPitch], int row0
 // What the state decays by from one token to another, log2.
 __device__ __forceinline__ float log2_between(float2 from, float2 to) { return (to.x - from.x) + (to.y - from.y); }
 
-// x as three bf16 values, two neighbours at a time.
+// x as two or three bf16 values, two neighbours at a time.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack_bf(a, b);
+    lo = pack_bf(a - bf_lo(hi), b - bf_hi(hi));
+}
 __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
     hi = pack_bf(a, b);
     a -= bf_lo(hi); b -= bf_hi(hi);
@@ -344,8 +348,10 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
 #pragma unroll
         for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + (k * kBlocks + n) * 512) = make_uint4(s[k][0], s[k][1], s[k][2], s[k][3]);
         operand_pairs(sm.M, mi * 16, ki * 16, lane, v);
-        *reinterpret_cast<uint4*>(to_M + n * 512) =
-            make_uint4(pack_bf(v[0].x, v[0].y), pack_bf(v[1].x, v[1].y), pack_bf(v[2].x, v[2].y), pack_bf(v[3].x, v[3].y));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split2(v[e].x, v[e].y, s[0][e], s[1][e]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to_M + k * kMPart + n * 512) = make_uint4(s[k][0], s[k][1], s[k][2], s[k][3]);
     }
 }
 
@@ -356,17 +362,17 @@ constexpr int kChainThreads = 256;   // warps 0-3: the state's products; warps 4
 template <int DK>
 struct ChainStage {
     unsigned char k[Q * DK * 2], q[Q * DK * 2];   // boxes of 64 values x 64 rows, 128-byte swizzle
-    unsigned char T[kTBytes], M[kMBytes];
+    unsigned char T[kTBytes], M[kMPart];   // M's leading part; the output warps fetch the other one themselves, there is no room for it
     __nv_bfloat16 v[Q][kSlice];
     float2 ef[Q];   // decay from the chunk's start to a row, from the row to the chunk's end
-    unsigned char pad[1024 - (kTBytes + kMBytes + Q * kSlice * 2 + Q * 8) % 1024];
+    unsigned char pad[1024 - (kTBytes + kMPart + Q * kSlice * 2 + Q * 8) % 1024];
 };
 template <int DK>
 struct ChainSmem {
     static constexpr int kRow = kSlice + 8;                // values of a row of the operands below, padded against bank conflicts
     ChainStage<DK> stage[kStages];
     float4 part[4][3][kSlice / 8][32];                     // K S^T over a warp's share of d_k, for the warps of the other row tiles
-    __nv_bfloat16 S[2][kSlice][DK];                        // leading part of the incoming state, by parity of the chunk; 16-byte units XOR-ed with the row index
+    __nv_bfloat16 S[2][2][kSlice][DK];                     // leading two parts of the incoming state, by parity of the chunk; 16-byte units XOR-ed with the row index
     __nv_bfloat16 R[3][Q][kRow];                        // V - e^G (K S^T), split in three
     __nv_bfloat16 W[3][Q][kRow];                        // e^{G_end - G} X, split in three
     __nv_bfloat16 X[2][2][Q][kRow];                     // X, split in two, by parity
@@ -433,7 +439,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         ChainStage<DK>& s = sm.stage[n % kStages];
         uint64_t* bar = &sm.full[n % kStages];
         const size_t ch = (size_t)(first + n) * H + head;
-        mbar_expect_tx(bar, 2 * Q * DK * 2 + kTBytes + kMBytes + Q * kSlice * 2 + Q * 8);
+        mbar_expect_tx(bar, 2 * Q * DK * 2 + kTBytes + kMPart + Q * kSlice * 2 + Q * 8);
 #pragma unroll
         for (int h = 0; h < DK / 64; ++h) {
             tma_box(s.k + h * 8192, &maps.k, khead * DK + 64 * h, s0 + n * Q, bar);
@@ -441,7 +447,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         }
         tma_box(s.v, &maps.v, col, s0 + n * Q, bar);
         bulk_load(s.T, ws.T + ch * kTBytes, kTBytes, bar);
-        bulk_load(s.M, ws.M + ch * kMBytes, kMBytes, bar);
+        bulk_load(s.M, ws.M + ch * kMBytes, kMPart, bar);
         bulk_load(s.ef, ws.ef + ch * Q, Q * 8, bar);
     };
     if (tid == kChainThreads - 32)
@@ -479,7 +485,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                     S[ms][nd][0] = a.x; S[ms][nd][1] = a.y; S[ms][nd][2] = b.x; S[ms][nd][3] = b.y;
                 }
         }
-        // The state as operands: part, tile of 8 rows, tile of 8 columns; its leading part goes to the output warps too.
+        // The state as operands: part, tile of 8 rows, tile of 8 columns; its leading parts go to the output warps too.
         uint32_t sp[3][NT][ND];
         auto split_state = [&](int parity) {
 #pragma unroll
@@ -490,7 +496,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                     for (int h = 0; h < 2; ++h) {
                         const int n = 2 * ms + h, row = n * 8 + g, unit = warp * ND + nd;
                         split3(S[ms][nd][2 * h], S[ms][nd][2 * h + 1], sp[0][n][nd], sp[1][n][nd], sp[2][n][nd]);
-                        *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[parity][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = sp[0][n][nd];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            *reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(&sm.S[parity][k][row][0]) + ((unit ^ (row & 7)) * 16) + t2 * 2) = sp[k][n][nd];
                     }
         };
         split_state(0);
@@ -625,9 +633,9 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                         split3(v0 * fr[i][h], v1 * fr[i][h], w[0], w[1], w[2]);
 #pragma unroll
                         for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(&sm.W[k][row][cc]) = w[k];
-                        const uint32_t hi = pack_bf(v0, v1);
-                        *reinterpret_cast<uint32_t*>(&sm.X[c & 1][0][row][cc]) = hi;
-                        *reinterpret_cast<uint32_t*>(&sm.X[c & 1][1][row][cc]) = pack_bf(v0 - bf_lo(hi), v1 - bf_hi(hi));
+                        split2(v0, v1, w[0], w[1]);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint32_t*>(&sm.X[c & 1][k][row][cc]) = w[k];
                     }
             uint32_t kc[ND / 2][4];   // key columns of the warp's share of the state, 16 tokens at a time
             auto load_keys = [&](int ki) {
@@ -644,7 +652,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 }
             };
             load_keys(0);
-            failed = __syncthreads_or(!here);   // W, X and the state's leading part are there; the output warps are done with the chunk before
+            failed = __syncthreads_or(!here);   // W, X and the state's leading parts are there; the output warps are done with the chunk before
             if (failed) break;                  // a copy did not arrive in time
             float m[MS][ND][4];
 #pragma unroll
@@ -693,8 +701,12 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
         for (; c < nck; ++c) {
             const ChainStage<DK>& s = sm.stage[c % kStages];
             const int t0 = s0 + c * Q, rows = len - c * Q;
+            uint32_t qr[KS][4], mr[4][4], ml[4][4], zr[NT][2];
+            const unsigned char* M_low = ws.M + ((size_t)(first + c) * H + head) * kMBytes + kMPart + (mt * (mt + 1) / 2) * 512 + lane * 16;
+#pragma unroll
+            for (int ki = 0; ki < 4; ++ki)
+                if (ki <= mt) *reinterpret_cast<uint4*>(ml[ki]) = *reinterpret_cast<const uint4*>(M_low + ki * 512);
             arrive(c);
-            uint32_t qr[KS][4], mr[4][4], zr[NT][2];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) rows_operand(qr[ks], s.q, mt, ks);
             const uint32_t sM = smem_u32(s.M) + (mt * (mt + 1) / 2) * 512 + lane * 16;
@@ -711,7 +723,7 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 }
             }
             const float e0 = s.ef[r0].x * p.L.scale, e1 = s.ef[r1].x * p.L.scale;
-            failed = __syncthreads_or(!here);   // X and the state's leading part are there
+            failed = __syncthreads_or(!here);   // X and the state's leading parts are there
             if (failed) break;
             if (tid == kChainThreads - 32 && c > 0 && c - 1 + kStages < nck) fetch(c - 1 + kStages);   // all warps are done with the chunk before
             // O = scale e^G (Q S^T) + M X
@@ -722,28 +734,34 @@ __global__ void __launch_bounds__(kChainThreads, 1) gdr_chain(const GdrPrefillAr
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
             const uint32_t sS = smem_u32(sm.S[c & 1]), sX = smem_u32(sm.X[c & 1]);
 #pragma unroll
-            for (int k2 = 0; k2 < KS / 2; ++k2)
+            for (int k = 1; k >= 0; --k)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t b[4];
-                    const int row = n * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
-                    ldsm4(b, sS + row * (DK * 2) + ((unit ^ (row & 7)) * 16));
-                    mma16816(o[n], qr[2 * k2], b[0], b[1]);
-                    mma16816(o[n], qr[2 * k2 + 1], b[2], b[3]);
-                }
+                for (int k2 = 0; k2 < KS / 2; ++k2)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t b[4];
+                        const int row = n * 8 + (lane & 7), unit = 4 * k2 + (lane >> 3);
+                        ldsm4(b, sS + (k * kSlice + row) * (DK * 2) + ((unit ^ (row & 7)) * 16));
+                        mma16816(o[n], qr[2 * k2], b[0], b[1]);
+                        mma16816(o[n], qr[2 * k2 + 1], b[2], b[3]);
+                    }
 #pragma unroll
             for (int n = 0; n < NT; ++n) { o[n][0] *= e0; o[n][1] *= e0; o[n][2] *= e1; o[n][3] *= e1; }
 #pragma unroll
             for (int ki = 0; ki < 4; ++ki)
                 if (ki <= mt) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                    for (int k = 1; k >= 0; --k)
 #pragma unroll
                         for (int n2 = 0; n2 < NT / 2; ++n2) {
                             uint32_t b[4];
                             ldsm4t(b, sX + ((k * Q + ki * 16 + (lane & 15)) * kRow + n2 * 16 + (lane >> 4) * 8) * 2);
                             mma16816(o[2 * n2], mr[ki], b[0], b[1]);
                             mma16816(o[2 * n2 + 1], mr[ki], b[2], b[3]);
+                            if (k == 0) {
+                                mma16816(o[2 * n2], ml[ki], b[0], b[1]);
+                                mma16816(o[2 * n2 + 1], ml[ki], b[2], b[3]);
+                            }
                         }
                 }
 #pragma unroll
