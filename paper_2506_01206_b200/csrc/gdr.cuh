@@ -44,10 +44,10 @@ cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int
 
 // Scratch of the chunked encode, per (chunk, value head).
 constexpr uint32_t kGdrTBytes = 15360, kGdrMBytes = 10240;  // lower triangles in 16 x 16 blocks, as the chain's lanes hold them (T in three parts, M in two)
-constexpr uint32_t kGdrWideTBytes = 24576, kGdrWideMBytes = 8192;   // the wide chain's: 64 rows of 128 bytes, 128-byte swizzle (three of them for T)
+constexpr uint32_t kGdrWideTBytes = 24576, kGdrWideMBytes = 16384;   // the wide chain's: 64 rows of 128 bytes, 128-byte swizzle, for each part
 struct GdrChunkWs {
     unsigned char* T;   // (1 + A)^-1 diag(beta), split into three bf16 values
-    unsigned char* M;   // masked products of queries and keys, split into two bf16 values; for the wide chain times T, one bf16 value
+    unsigned char* M;   // masked products of queries and keys, split into two bf16 values; for the wide chain times T
     float2* ef;         // decays of 64 rows: from the chunk's start, to its end
     float* o;           // (T, Hv * d_v) fp32 outputs before the norm; NULL: there is no norm, or the chain does it
 };

@@ -24,8 +24,9 @@
 //
 // Precision.  States keep fp32 accuracy: q, k, v are bf16 as given; everything else that meets them in a product of the state's path (S, T, the
 // differences, X) is split into three bf16 values (24 bits), which costs three products with an exact operand and six where both are
-// split.  Two values (16 bits) left an error of 3e-6 in the states.  The outputs' products take S and M as one bf16 value and X as two: what they lose is the size
-// of the outputs' own rounding.  Running log decays are summed in 64 bits and kept as two fp32 values, as differences of sums of 10^4 are wanted to 2^-24.
+// split.  Two values (16 bits) left an error of 3e-6 in the states.  The outputs' products take S, M and X (the wide chain: S, M T
+// and V - e^G (K S^T)) as two values each: what they lose is 2^-16 of the products' sizes, which shows in bf16 outputs only where the products cancel to a hundredth.  With one
+// value the largest errors were ten steps of a result there.  Running log decays are summed in 64 bits and kept as two fp32 values, as differences of sums of 10^4 are wanted to 2^-24.
 //
 // Kernel 2 runs on the warp-level tensor instructions (mma.sync), not on tcgen05: its products are 64 x 16 x 128 and depend on
 // one another, so what counts is the way from one to the next (registers to shared memory and back, a barrier) and not the rate.
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
     }
     __syncthreads();
     if (kWide) {
-        // Rows of 64 values: T in three parts, M T diag(beta).  A thread takes eight columns of rows lane and lane + 32; columns u and 7 - u, so that every warp has as
+        // Rows of 64 values: T in three parts, M T diag(beta) in two.  A thread takes eight columns of rows lane and lane + 32; columns u and 7 - u, so that every warp has as
         // much of the triangle.
         unsigned char* to_T = ws.T + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideTBytes;
         unsigned char* to_M = ws.M + ((size_t)cidx * p.L.n_v_heads + head) * kGdrWideMBytes;
@@ -318,19 +319,20 @@ __global__ void __launch_bounds__(kPrepThreads) gdr_chunk_prepare(const GdrPrefi
             for (int r = 0; r < 2; ++r) {
                 const int i = lane + 32 * r;
                 const uint32_t to = (uint32_t)i * 128 + (uint32_t)((u ^ (i & 7)) * 16);
-                uint4 t[3], m;
-                uint32_t *th = &t[0].x, *tm = &t[1].x, *tl = &t[2].x, *mm = &m.x;
+                uint4 t[3], m[2];
+                uint32_t *th = &t[0].x, *tm = &t[1].x, *tl = &t[2].x, *mh = &m[0].x, *ml = &m[1].x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 x = *reinterpret_cast<const float2*>(&sm.A[i][c + 2 * e]);
                     split3(c + 2 * e <= i ? x.x * b[2 * e] : 0.f, c + 2 * e + 1 <= i ? x.y * b[2 * e + 1] : 0.f, th[e], tm[e], tl[e]);
                     float p0, p1;
                     unpk(acc[r][e], p0, p1);
-                    mm[e] = pack_bf(p0 * b[2 * e], p1 * b[2 * e + 1]);
+                    split2(p0 * b[2 * e], p1 * b[2 * e + 1], mh[e], ml[e]);
                 }
 #pragma unroll
                 for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to_T + k * 8192 + to) = t[k];
-                *reinterpret_cast<uint4*>(to_M + to) = m;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to_M + k * 8192 + to) = m[k];
             }
         }
         return;

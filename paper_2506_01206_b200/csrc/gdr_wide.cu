@@ -39,15 +39,14 @@ struct WideStage {
     unsigned char k[Q * DK * 2], q[Q * DK * 2];   // boxes of 64 values x 64 rows, 128-byte swizzle
     unsigned char T[kGdrWideTBytes], M[kGdrWideMBytes];   // 64 x 64 in rows of 128 bytes, 128-byte swizzle
     __nv_bfloat16 v[Q][DV];
-    float2 ef[Q];                // decay from the chunk's start to a row, from the row to the chunk's end
-    unsigned char pad[512];
 };
 template <int DK, int DV>
 struct WideSmem {
     WideStage<DK, DV> stage[kStages];
+    float2 ef[kStages][Q];       // of a stage too: decay from the chunk's start to a row, from the row to the chunk's end
     __nv_bfloat16 z[Q][DV];      // gate
     float eo[Q];                 // decay from the chunk's start times scale, for the output warps (which may fall behind the stages)
-    float o[Q][DV + 4];          // outputs on their way from a lane per value to a row per warp
+    float o[Q][DV];              // outputs on their way from a lane per value to a row per warp
     uint64_t full[kStages], done[kStages];                   // copies of a stage, all products that read it (and, through w, all that the state warps read of it)
     uint64_t state[2], r[2], w[2], free_o;                   // operands are in tensor memory (in two portions), output accumulators have been read
     uint64_t mma1, mma2, out, last;                          // products
@@ -66,8 +65,8 @@ __device__ __forceinline__ bool elect_one() {
     return r != 0;
 }
 
-// Two neighbours as three bf16 values each.  The first is rounded (the outputs take it alone), the others are truncated: the remainders are exact, and 8 + 8 + 8
-// bits hold all 24 of a fp32 value.
+// Two neighbours as three bf16 values each.  The first is rounded, the others are truncated: the remainders are exact, and 8 + 8 + 8
+// bits hold all 24 of a fp32 value.  The outputs take the first two, 2^-15 of a value.
 __device__ __forceinline__ uint32_t leading_halves(u64 v) { return __byte_perm((uint32_t)v, (uint32_t)(v >> 32), 0x7632); }
 __device__ __forceinline__ uint32_t split_first(u64& v) {   // leaves the remainder
     float a, b;
@@ -178,7 +177,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
         for (int c = 0; c < nck; ++c) {
             WideStage<DK, DV>& s = sm.stage[c % kStages];
             // The thread takes eight tokens of the first half of the chunk and the eight that lie 32 further on, and hands them over in that order.
-            const float2* ef = s.ef + 8 * part;
+            const float2* ef = sm.ef[c % kStages] + 8 * part;
             const int rows = len - c * Q, mine = rows - 8 * part;
             wait(&sm.full[c % kStages], c / kStages);
             uint32_t vv[8];   // values of two tokens each
@@ -249,7 +248,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
             wait(&sm.mma2, c);
             tc_fence_after();
             load_d1();
-            const float all = s.ef[Q - 1].x;
+            const float all = sm.ef[c % kStages][Q - 1].x;
 #pragma unroll
             for (int hand = 0; hand < 2; ++hand) {
                 u64 x[4];
@@ -395,8 +394,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
             }
             if (ok && elect_one()) {
 #pragma unroll
-                for (int k = 0; k < DK / 16; ++k)
-                    mma_bf16_ts(tmem + kDQ, tmem + kS + k * 8, dQ + (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4), idTok, k > 0);
+                for (int part = 1; part >= 0; --part)
+#pragma unroll
+                    for (int k = 0; k < DK / 16; ++k)
+                        mma_bf16_ts(tmem + kDQ, tmem + kS + part * (DK / 2) + k * 8, dQ + (uint64_t)(((k >> 2) * 8192 + (k & 3) * 32) >> 4), idTok, part < 1 || k > 0);
             }
             __syncwarp();
             // X = R T^T: the six products of parts that reach 24 bits, small ones first
@@ -413,10 +414,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                     tokens(kD1, 0, dT, 0, hand, true);
                     if (hand == 1) {
                         mma_commit(&sm.mma2);
-                        tokens(kDO, 1, dM, 0, 0, false);
-                        tokens(kDO, 0, dM, 0, 0, true);
-                        tokens(kDO, 1, dM, 0, 1, true);
-                        tokens(kDO, 0, dM, 0, 1, true);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {   // the three products of parts that reach 16 bits
+                            tokens(kDO, 1, dM, 0, h, h > 0);
+                            tokens(kDO, 0, dM, 1, h, true);
+                            tokens(kDO, 0, dM, 0, h, true);
+                        }
                         mma_commit(&sm.out);
                     }
                 }
@@ -457,7 +460,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) gdr_chain_wide(const GdrPrefi
                 tma_box(s.v, &maps.v, head * DV, s0 + c * Q, bar);
                 bulk_load(s.T, ws.T + ch * kGdrWideTBytes, kGdrWideTBytes, bar);
                 bulk_load(s.M, ws.M + ch * kGdrWideMBytes, kGdrWideMBytes, bar);
-                bulk_load(s.ef, ws.ef + ch * Q, Q * 8, bar);
+                bulk_load(sm.ef[c % kStages], ws.ef + ch * Q, Q * 8, bar);
             }
             __syncwarp();
         }

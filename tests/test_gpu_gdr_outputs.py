@@ -57,3 +57,44 @@ def test_the_same_tokens_in_chunks_and_token_by_token():
     want, _, o, size, size64 = gdr.encode(**p.args(), cu=[0, 64], sizes=True)
     check(p, a, want, o, STATE * size)
     check(p, b, want, o, STATE * size + CHUNKED * size64)
+
+
+# ---------------------------------------------------------------- the wide chain
+# Its outputs are scale e^G (S q) + (M T) R with R = V - e^G (K S^T) and T the inverse of the chunk's triangle: other products than M X, though the same sum.  The second
+# parts of S and R are truncated, 2^-7 of 2^-8; M T is rounded twice, 2^-16; the product of the second parts of M T and R is left out, 2^-16.
+WIDE_S, WIDE_MT = 2.0 ** -15, 2.0 ** -15 + 2 * 2.0 ** -16
+
+
+def wide_sizes(p, cu, S0):
+    """(T, Hv, d_v): sums of the sizes of the products of either sum, in 64 bits, a chunk at a time by the closed form."""
+    a = {n: None if v is None else np.asarray(v, np.float64) for n, v in p.args().items() if n in ("q", "k", "v", "dt", "beta", "A", "dt_bias")}
+    x = np.logaddexp(0.0, a["dt"] + a["dt_bias"]) * a["A"]
+    beta, scale, dk, dv = 1 / (1 + np.exp(-a["beta"])), p.dk ** -0.5, p.dk, p.dv
+    of_s, of_mt = np.zeros((p.rows, p.hv, dv)), np.zeros((p.rows, p.hv, dv))
+    for s in range(len(cu) - 1):
+        for h in range(p.hv):
+            S = np.zeros((dv, dk)) if S0 is None else np.asarray(S0, np.float64).reshape(-1, p.hv, dv, dk)[s, h]
+            g = slice(h // (p.hv // p.hk) * dk, (h // (p.hv // p.hk) + 1) * dk)
+            for t in range(int(cu[s]), int(cu[s + 1]), 64):
+                r = slice(t, min(t + 64, int(cu[s + 1])))
+                q, k, v, b, G = a["q"][r, g], a["k"][r, g], a["v"][r, h * dv:(h + 1) * dv], beta[r, h], np.cumsum(x[r, h])
+                between = np.tril(np.exp(np.minimum(G[:, None] - G, 0)))
+                T = np.linalg.inv(np.eye(len(G)) + np.tril(b[:, None] * between * (k @ k.T), -1)) * b
+                M, R = scale * between * (q @ k.T), v - np.exp(G)[:, None] * (k @ S.T)
+                of_s[r, h], of_mt[r, h] = scale * np.exp(G)[:, None] * (np.abs(q) @ np.abs(S).T), np.abs(M @ T) @ np.abs(R)
+                S = np.exp(G[-1]) * S + (np.exp(G[-1] - G)[:, None] * (T @ R)).T @ k
+    return of_s, of_mt
+
+
+MANY = [(38, 38, 128, 128), (13, 39, 64, 128), (5, 80, 128, 64), (76, 76, 64, 64)]   # plan_gdr (csrc/api.cu): a whole head per block
+
+
+@pytest.mark.parametrize("hk,hv,dk,dv", MANY)
+@pytest.mark.parametrize("lens,init,gate,norm", [([200], True, True, True), ([65], False, False, False), ([64, 1, 70], True, False, True)])
+def test_wide_chain(hk, hv, dk, dv, lens, init, gate, norm):
+    p = Problem(sum(lens), hk, hv, dk, dv, gate=gate, norm=norm, seed=93 + sum(lens))
+    assert is_chunked(p, lens)
+    cu, h0, out, states = run_encode(p, lens, init)
+    want, _, o, size = gdr.encode(**p.args(), cu=cu, S0=h0, sizes=True)[:4]
+    of_s, of_mt = wide_sizes(p, cu, h0)
+    check(p, out, want, o, STATE * (size + of_s + of_mt) + WIDE_S * of_s + WIDE_MT * of_mt)
