@@ -468,7 +468,8 @@ typedef struct {
  *   no sequence may start from another's final_slot, however long it is.  init_slot[s] == final_slot[s] is allowed.  Rows that belong to no sequence
  *   are neither read into a result nor written
  *   max_seqlen: an upper bound on the longest sequence (HOST value): with its help the call chooses how it works; the results do not
- *               depend on it beyond rounding
+ *               depend on it beyond rounding: states are as good as fp32 arithmetic makes them, outputs are off by their own rounding and, where a long bf16 sequence's
+ *               products cancel, by 2^-14 of the products' sizes
  *   workspace : device scratch of at least mdraft_gdr_prefill_workspace_bytes(...) bytes, 256-byte aligned; NULL where that is 0.  Its contents
  *               need not be initialised; calls that may run at the same time (other streams, graphs replayed side by side) each need their own.
  *               `out` must not overlap an input, and no two sequences may end in one slot

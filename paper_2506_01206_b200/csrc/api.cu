@@ -1030,8 +1030,10 @@ GdrLayerDev gdr_layer_dev(const mdraft_gdr_layer* L) {
 
 // How an encode is done: token by token, or in chunks; there a chain's block takes 16 values of a head, or all of them.
 // A narrow block is done with a chunk in half the time of a wide one, which does eight times its work: narrow as long as two waves of them hold the call.
-// Measured (2048 tokens, 128 x 128, narrow against wide): 8 heads 77 against 187 us, 20 heads 145 against 197, 36 heads 162 against 208, 40 heads 223 against
-// 212; 64 values a head: 72 heads 183 against 206, 100 heads 263 against 226; 8 sequences of 64-128 tokens x 12 heads 49 against 30.
+// Measured (2048 tokens, 128 x 128, narrow against wide): 8 heads 77 against 190 us, 20 heads 149 against 200, 36 heads 167 against 217, 40 heads 231 against
+// 219; 64 values a head: 72 heads 190 against 218, 100 heads 273 against 239; 8 sequences of 64-128 tokens x 12 heads 48 against 33.
+// The rule counts sequences and does not see their lengths (they are on the device): one long one beside many short ones is taken wide, where narrow would do better (12
+// heads, 32768 tokens beside three sequences of 5: 1.14 ms narrow, 2.85 wide; 8192 beside seven of 64: 0.30 against 0.73).
 struct GdrPlan {
     bool chunked;
     int n_chunks_bound, slice;
@@ -1039,9 +1041,9 @@ struct GdrPlan {
 };
 
 // The longest sequence that is done token by token.  A token takes 0.12 to 0.16 us there, the shortest call in chunks 14 us; with more heads and sequences both grow, token
-// by token earlier.  Measured (bf16, 128 x 128, token by token against chunks): 12 heads 33 tokens 8.7 against 13.6 us, 64 11.9 against 14.9, 96 16.0 against 16.8; four
-// sequences of 33 tokens 14.7 against 21.6, 64 21.7 against 22.1, 96 30.0 against 27.3; eight (more than gdr_few_rows) 24 tokens 17.2 against 23.0, 33 22.8
-// against 23.5, 48 28.7 against 23.6.  The least favourable: four sequences of 64 tokens x 4 heads, 16.0 against 15.0.
+// by token earlier.  Measured (bf16, 128 x 128, token by token against chunks): 12 heads 33 tokens 9.4 against 14.0 us, 64 12.5 against 15.2, 96 16.7 against 17.4; four
+// sequences of 33 tokens 14.9 against 22.4, 64 22.0 against 22.8, 96 30.7 against 28.0; eight (more than gdr_few_rows) 24 tokens 17.6 against 23.4, 33 22.9
+// against 24.0, 48 29.1 against 24.1.  The least favourable: four sequences of 64 tokens x 4 heads, 16.5 against 15.4.
 int gdr_sequential_max(const mdraft_gdr_layer* L, int n_seq) { return gdr_few_rows(L->n_v_heads, L->d_v, n_seq) ? 64 : 32; }
 
 GdrPlan plan_gdr(const mdraft_gdr_layer* L, int T, int n_seq, int max_seqlen) {

@@ -36,9 +36,9 @@ struct GdrPrefillArgs {
 };
 
 // Token by token: one kernel, no workspace.  Blocks hold 16 rows of a state where the call has few of them, else 32: 16 rows are one warp to a scheduler, whose tokens take
-// 0.12 us instead of 0.16, but the same work is more blocks and more copies of a head's keys.  Measured (16 against 32 rows; 128 x 128): 12 heads x 32 tokens 7.7
-// against 9.7 us, fp32 512 tokens 72 against 108, four such 159 against 201; six sequences of 512 in fp32 (3.9 blocks of 16 to an SM) 307 against 305. Beyond, 16 rows lose: eight
-// sequences of 32 tokens (5.2 blocks to an SM) 23.5 against 21.0, eight of 512 in fp32 333 against 312.
+// 0.12 us instead of 0.16, but the same work is more blocks and more copies of a head's keys.  Measured (16 against 32 rows; 128 x 128): 12 heads x 32 tokens 8.3
+// against 10.4 us, fp32 512 tokens 72 against 109, four such 160 against 202; six sequences of 512 in fp32 (3.9 blocks of 16 to an SM) 305 against 305. Beyond, 16 rows lose: eight
+// sequences of 32 tokens (5.2 blocks to an SM) 23.6 against 21.1, eight of 512 in fp32 325 against 305.
 inline bool gdr_few_rows(int n_v_heads, int d_v, int n_seq) { return (int64_t)n_v_heads * (d_v / 16) * n_seq <= 4 * sm_count(); }
 cudaError_t launch_gdr_sequential(const GdrPrefillArgs& p, int d_k, int d_v, int act, cudaStream_t st);
 
@@ -76,7 +76,7 @@ cudaError_t launch_gdr_step(const GdrStepArgs& p, int d_k, int d_v, int act, cud
 
 // ---------------------------------------------------------------- device helpers shared by the kernels
 // 2^(hi + lo) to about one unit of the last place (the hardware's 2^x is off by up to four): a decay is multiplied into the state token after token or chunk after
-// chunk, so what it is off by adds up over as many as a head remembers.  hi = n + f, and e^y, y = (f + lo) ln 2, by its Taylor series (|y| <= 0.347: what follows y^7 / 7! is
+// chunk, so what it is off by adds up over as many as a head remembers (state of 400 fp32 tokens off by 1.4e-6 with the hardware's functions, 2.8e-7 with these).  hi = n + f, and e^y, y = (f + lo) ln 2, by its Taylor series (|y| <= 0.347: what follows y^7 / 7! is
 // below 6e-9).  2^n comes in two factors, as n may go past the exponent's range either way.
 __device__ __forceinline__ float exp2_f32(float hi, float lo) {
     hi = hi < -252.f ? -252.f : (hi > 252.f ? 252.f : hi);   // (a NaN stays one)

@@ -16,9 +16,9 @@
 //   1. gdr_chunk_prepare, a block per (value head, chunk): [K; Q] K^T as one product of 128 rows on the tensor cores (tcgen05, operands by
 //      TMA), then the triangle's inverse in fp32: its diagonal blocks of 16 by forward substitution, a column per lane, the blocks below by two rounds of
 //      products (of the 16s, of the 32s).  Results go to the workspace in the order in which kernel 2's lanes hold them.  Bound by shared-memory
-//      latency: 2048 tokens x 12 heads 13 us, 141000 x 12 0.65 ms (for the wide chain, with M T).
+//      latency: 2048 tokens x 12 heads 13 us, 141000 x 12 0.69 ms (for the wide chain, with M T: 64^3 multiply-adds of a chunk and head out of shared memory, which is 84 % busy).
 //   2. gdr_chain, a block per (slice of 16 values, value head, sequence): state in registers, three small products per chunk one after another
-//      (K S^T; T times the difference; the update), beside them the two of the outputs.  2048 tokens: 64 us, 2 us a chunk whatever the width up to the SMs' number
+//      (K S^T; T times the difference; the update), beside them the two of the outputs.  2048 tokens: 66 us, 2 us a chunk whatever the width up to the SMs' number
 //      of blocks.  Where there are many chains a block takes a whole head instead (gdr_wide.cu).
 //   3. gdr_norm_gate where there is an output norm, which needs all slices of a row (the wide chain does it itself).  10 us for 2048 tokens x 12 heads.
 //

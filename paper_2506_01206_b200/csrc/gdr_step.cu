@@ -11,7 +11,8 @@
 // The tree step is memory traffic: 64 KB read and 64 KB written per node and head of 128 x 128.  A block takes one head of one
 // node, 256 threads with four rows per lane group, all of whose loads are in flight before the first is used.  The fork is the gather itself
 // (read slot parent_slot[i], write slot node_slot[i]).  Levels of a call are chained by programmatic dependent launch: slots, constants and
-// input rows are fetched while the level ahead still runs.  Measured (12 heads of 128 x 128, bf16): 32 sequences x 32 nodes in 5 to 9 levels 212 us, 5.4 TB/s of the
+// input rows are fetched while the level ahead still runs; decay and write strength are formed while the states are on their way (ahead of their loads: 10 % more time; by one warp
+// for the block: 20 %).  Measured (12 heads of 128 x 128, bf16): 32 sequences x 32 nodes in 5 levels 214 us, 5.4 TB/s of the
 // states that have to move; a round of 150 nodes in 6 levels 43 us, bound by the latency of its small levels.
 //
 // The token-by-token encode keeps the state in registers for the whole sequence; 16 or 32 rows to a block, so that a head of 128 rows is
@@ -165,7 +166,7 @@ struct SeqSmem {
 };
 
 // Blocks to an SM: as many as the registers allow without spills (a token's operands wait as they lie in memory, which for bf16 halves them: eight sequences of up to 9
-// tokens x 12 heads 10.7 -> 8.5 us, as three blocks of 384 threads fit instead of two).
+// tokens x 12 heads a fifth less time, 8.9 us, as three blocks of 384 threads fit instead of two).
 template <typename T, int DK, int R>
 constexpr int kSeqBlocks = R == 32 ? (DK == 64 || sizeof(T) == 2 ? 3 : 2) : (DK == 64 || sizeof(T) == 2 ? 4 : 3);
 
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(8 * R + kHelpers, kSeqBlocks<T, DK, R>) gdr_se
                 beta_next = s.beta[t];
             };
             fetch_next(0);
-#pragma unroll 8   // (against 2: 56.8 -> 51.2 us for 480 tokens of 64 values)
+#pragma unroll 8   // (against 2: a tenth less time for 480 tokens of 64 values, 52.6 us)
             for (int t = 0; t < n; ++t) {
 #pragma unroll
                 for (int i = 0; i < KI; ++i) { k[i] = widen(k_next[i]); q[i] = widen(q_next[i]); }

@@ -9,11 +9,11 @@
 //     O  = scale e^G (S Q^T) + R (M T)^T
 //
 // S itself stays in registers (fp32), the operands of the other side (K, Q, T, M T) come by TMA as they are used.  M T instead of M makes the outputs
-// wait for R, not for X.  Three products of a chunk depend on one another; in between 256 threads take accumulators to operands: tensor
-// memory -> registers -> tensor memory.  A chunk of 128 x 128 costs 9000 cycles, 11000 with all SMs at work, of which the products are 2300; the rest is the way between them, where the
-// splitting into three parts alone takes 16 cycles of a scheduler per pair of values and warp.  With as many chains as SMs or more that beats the narrow chain, whose
-// blocks share a head among eight SMs to be done with a chunk in 3900 (measured where the choice is made).  32 sequences of 1000 to 8000 tokens x 12 heads: 1.18 ms for
-// the chain and 0.65 ms for the triangles ahead of it, 1.9 ms in all against 10.7 token by token.
+// wait for R, not for X.  Three products of a chunk depend on one another; in between 512 threads take accumulators to operands: tensor
+// memory -> registers -> tensor memory.  A chunk of 128 x 128 costs 9500 cycles, 11000 with all SMs at work; the tensor pipe is busy for a third of that (ncu), the rest is the way between
+// the products, on which the warps wait for tensor memory and for loads above all.  With as many chains of like length as SMs or more that beats the narrow chain, whose
+// blocks share a head among eight SMs to be done with a chunk in 3900 (measured where the choice is made).  32 sequences of 1000 to 8000 tokens x 12 heads: 1.17 ms for
+// the chain and 0.69 ms for the triangles ahead of it (cold, one behind the other), 2.0 ms in all, call after call, against 10.7 token by token.
 //
 // Warps 0-15: the state's, warps w, w + 4, .. share rows 32 (w % 4) .. and split the columns.  Four warps: outputs (norm and gate inside).  One warp issues the
 // products, one the copies, one those of the gate.  All waits on mbarriers are bounded; a thread whose wait has run out goes on through the block's barriers without

@@ -8,7 +8,8 @@
 // either half in a lane (two loads of 8 or 16 bytes), so that it takes none.  The turns of a row (position times frequency, reduced
 // to [-1/2, 1/2] turns in 64 bits, as an fp32 product is off by whole radians at positions of a million) are formed once and shared by its heads
 // through shared memory.  A block works through passes of rows and has the next one's loads in flight meanwhile.  Bound: memory.  Measured (bf16, 12 + 4 heads): heads of 64, 32
-// values turned, 141000 rows 112 us, 5.2 TB/s (200 us with one head per thread and pass, without loads ahead; issue slots are nearly as full); heads of 128, all turned, 2048 rows 8.2 us.
+// values turned, 141000 rows 112 us on the device (119 a call), 5.2 TB/s (200 us with one head per thread and pass, without loads ahead; issue slots are nearly as full); heads of 128, all turned, 2048 rows 6.2
+// us on the device (8.2 a call).
 #include "common.cuh"
 #include "qk_norm.cuh"
 
