@@ -253,3 +253,33 @@ def test_one_token_that_forgets_everything_leaves_the_decays_behind_it_exact(n, 
         w_out, w_states, o, size, size64 = gdr.encode(**p.args(), cu=[0, n], S0=h0, sizes=True)
     check_states(cache.ssm[0, 1], np.asarray(w_states)[0])
     p.check_out(out, w_out, o, size, size64 if is_chunked(p, [n]) else None)
+
+
+@pytest.mark.parametrize("act,n,hv", [("bf16", 24, 2), ("f32", 100, 2), ("bf16", 200, 2), ("bf16", 200, 40)])
+@pytest.mark.parametrize("which", ["k", "v", "dt", "beta"])
+def test_a_nan_reaches_every_token_behind_it(act, n, hv, which):
+    """As in the recurrence: no clamp, comparison or mask on the way of a decay, a strength or an operand takes it for a number."""
+    t = n // 2
+    p = Problem(n, 1, hv, act=act, gate=False, norm=False, seed=72)
+    p.np[which][t] = np.nan
+    p.upload()
+    cache, out = p.cache(1), p.out()
+    md.mdraft_gdr_prefill(p.layer, cache, 0, *p.dev, out, None, n, None, i32([0]), p.workspace(1, n))
+    torch.cuda.synchronize()
+    assert bool(out[t:].isnan().all()) and bool(cache.ssm.isnan().all())
+    assert bool(out[:t // 64 * 64].isfinite().all())
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("which", ["k", "v", "dt", "beta"])
+def test_a_nan_reaches_the_nodes_below_it(act, which):
+    p = Problem(4, 1, 2, act=act, gate=False, norm=False, seed=73)
+    p.np[which][1] = np.nan
+    p.upload()
+    cache, out = p.cache(5), p.out()
+    cache.ssm[0, 0] = torch.from_numpy(p.states(1)[0]).cuda()
+    md.mdraft_gdr_tree_step(p.layer, cache, 0, *p.dev, out, i32([0, 0, 1, 2]), i32([1, 2, 3, 4]), [0, 2, 4])   # nodes 0 and 1 below the root, 2 below 0, 3 below 1
+    torch.cuda.synchronize()
+    for node, bad in enumerate((False, True, False, True)):
+        assert bool(out[node].isnan().all() if bad else out[node].isfinite().all())
+        assert bool(cache.ssm[0, 1 + node].isnan().all() if bad else cache.ssm[0, 1 + node].isfinite().all())
